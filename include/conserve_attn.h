@@ -17,6 +17,7 @@
  *    address on the current HIP device; the caller owns that memory and keeps it alive until the
  *    stream reaches the call. Host pointers: cs_conv arrays, q_lens, and the out-parameters.
  *  - Element type: bf16 (IEEE binary32 with the low 16 bits dropped) everywhere; accumulation fp32.
+ *    A pool may hold K and V in 4 bits instead (cs_pool_create_as); what goes in and out stays bf16.
  *  - Append-then-attend: cs_kv_append is the only writer of a conversation's K/V. Attention calls
  *    take queries for the LAST q_len positions of each conversation; query i of a conversation of
  *    length L sits at position p = L - q_len + i and sees keys 0..p (itself included). Softmax
@@ -97,6 +98,31 @@ size_t cs_pool_workspace_bytes(const cs_pool_desc* desc);
 cs_status cs_pool_create(const cs_pool_desc* desc, void* kv_base, size_t kv_bytes, void* ws_base,
                          size_t ws_bytes, uint64_t placement_seed, cs_pool** out);
 
+/*
+ * What a pool's pages hold.
+ * CS_KV_BF16: K and V as they are appended (the layout above).
+ * CS_KV_FP4: K and V in 4 bits, 17 head_dim bytes a block instead of 64 head_dim: 3.76 times the tokens in
+ *   the same memory, and as many fewer bytes for a decode step to read and for a transfer to move. Values
+ *   are e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives) times a power of two: for K one for every 32
+ *   dims of a token and kv head, for V one for every token and kv head. With a the largest magnitude of
+ *   such a group the power is 2^(floor(log2 a) - 2), at least 2^-126; a value is rounded to the nearest
+ *   e2m1 value times it (ties to the even code) and at most to 6 times it. K and V must be finite: a group
+ *   with an infinity or NaN reads back as NaN. Attention is that of the held values: every call below does on
+ *   such a pool what it does on a bf16 one, with the same arguments, asynchrony and errors.
+ *   Block (layer, page, kv head), two codes a byte, the first in the low bits: K[4][16 tokens][d/4 dims] (part
+ *   i holds dims i d/4 .. of every token), V[4][16][d/16][4]: part i, row c, tile t hold dim 16 t + c of tokens
+ *   4 i .. 4 i + 3; then bytes e (the power 2^(e - 127)): K[d/32 groups][16 tokens], V[16 tokens], zeros up to
+ *   17 d. Token slots >= length are zeros.
+ */
+enum { CS_KV_BF16 = 0, CS_KV_FP4 = 1 };
+
+/* As cs_pool_kv_bytes and cs_pool_create, for a pool of the given format (CS_KV_BF16: the same as those;
+ * the workspace is cs_pool_workspace_bytes either way). cs_pool_kv_bytes_as returns 0 and cs_pool_create_as
+ * CS_EINVAL for an unknown format. */
+size_t cs_pool_kv_bytes_as(const cs_pool_desc* desc, int32_t format);
+cs_status cs_pool_create_as(const cs_pool_desc* desc, int32_t format, void* kv_base, size_t kv_bytes, void* ws_base,
+                            size_t ws_bytes, uint64_t placement_seed, cs_pool** out);
+
 /* Destroy host state; never frees caller memory. Waits for the pool's enqueued work first. */
 cs_status cs_pool_destroy(cs_pool* pool);
 
@@ -137,6 +163,67 @@ cs_status cs_kv_append(cs_pool* pool, cs_conv conv, int32_t n_new, const void* k
  */
 cs_status cs_kv_append_batch(cs_pool* pool, int32_t n_convs, const cs_conv* convs,
                              const int32_t* n_new, const void* k, const void* v, cs_stream stream);
+
+/*
+ * Rotary positions. Of every head the first rotary_dim dims turn with the token's position p (0 for a
+ * conversation's first token), pair i = 0 .. rotary_dim/2 - 1 by p inv_freq[i] radians:
+ *   (a, b) -> amplitude (a cos - b sin, a sin + b cos)
+ * where a pair is dims (i, i + rotary_dim/2), or (2 i, 2 i + 1) with interleaved; the other dims stay.
+ * The angle is exact to 2^-34 turns at any position; the rotated value is computed in fp32 and rounded
+ * once, to bf16 or to the pool's 4 bits.
+ */
+typedef struct {
+  int32_t rotary_dim;   /* 16, 32, .., head_dim */
+  int32_t interleaved;  /* 0 or 1 */
+  double amplitude;     /* factor on rotated dims */
+  double inv_freq[64];  /* radians per position; the first rotary_dim/2 are used */
+} cs_rope;
+
+/*
+ * Fill *out: inv_freq[i] = f_i = base^(-2 i / rotary_dim), amplitude 1, changed for contexts `factor` times
+ * longer than those a model was trained on (original_len tokens):
+ *   CS_ROPE_PLAIN   not at all (the last four arguments are not read)
+ *   CS_ROPE_LINEAR  f_i / factor
+ *   CS_ROPE_NTK     base factor^(rotary_dim / (rotary_dim - 2)) in place of base
+ *   CS_ROPE_PARTS   f_i (g + (1 - g) / factor) with g = (n - low) / (high - low), between 0 and 1, where pair i
+ *                   makes n = original_len f_i / 2 pi turns over the original context: pairs of fewer than
+ *                   `low_turns` turns slow down, of more than `high_turns` do not; amplitude 0.1 ln(factor) + 1
+ * A caller may change any field afterwards. Host only.
+ * Errors: CS_EINVAL (null, rotary_dim no multiple of 16 in 16 .. 128, interleaved not 0 or 1, base <= 1,
+ * unknown scaling, factor < 1, for PARTS original_len <= 0 or low_turns >= high_turns, not finite).
+ */
+enum { CS_ROPE_PLAIN = 0, CS_ROPE_LINEAR = 1, CS_ROPE_NTK = 2, CS_ROPE_PARTS = 3 };
+cs_status cs_rope_init(cs_rope* out, int32_t rotary_dim, int32_t interleaved, double base, int32_t scaling,
+                       double factor, double original_len, double low_turns, double high_turns);
+
+/*
+ * cs_kv_append_batch with rotated keys: a token's K enters the cache turned by its position. With q (may be
+ * null) the queries of the same tokens, [n_layers][sum(n_new)][n_q_heads][head_dim], are rotated in the same
+ * launch into q_out (same shape; q itself, or no overlap with it), ready for the attention calls.
+ * Errors: as cs_kv_append_batch; CS_EINVAL for a null or invalid rope (rotary_dim no multiple of 16 in
+ * 16 .. head_dim, interleaved not 0 or 1, amplitude or an inv_freq in use not finite), q without q_out.
+ */
+cs_status cs_kv_append_rope(cs_pool* pool, const cs_rope* rope, int32_t n_convs, const cs_conv* convs, const int32_t* n_new,
+                            const void* k, const void* v, const void* q, void* q_out, cs_stream stream);
+
+/*
+ * Queries of the last q_lens[i] positions of each conversation (those the attention calls take), rotated:
+ * q, out [n_layers][sum(q_lens)][n_q_heads][head_dim] for any n_layers >= 0; out may be q itself, otherwise
+ * they do not overlap. Errors: as cs_attn_extend, and as cs_kv_append_rope for rope; CS_EINVAL (n_layers < 0).
+ */
+cs_status cs_rope_q(cs_pool* pool, const cs_rope* rope, int32_t n_convs, const cs_conv* convs, const int32_t* q_lens,
+                    int32_t n_layers, const void* q, void* out, cs_stream stream);
+
+/*
+ * Read tokens [starts[i], starts[i] + n[i]) of each conversation back from the cache: k, v
+ * [n_layers][sum(n)][n_kv_heads][head_dim], conversations in batch order. A bf16 pool gives the bits that
+ * were appended (rotated, if they were); a 4-bit pool the values it holds, exact in bf16 (below 2^-126 in magnitude
+ * as far as bf16 holds them). The conversations must be distinct. n[i] == 0 is allowed.
+ * Errors: CS_EINVAL (null, negative, duplicate conversation, too many tokens), CS_ENOENT, CS_ERANGE (past
+ * the conversation's end), CS_EHIP.
+ */
+cs_status cs_kv_read(cs_pool* pool, int32_t n_convs, const cs_conv* convs, const int64_t* starts, const int32_t* n, void* k,
+                     void* v, cs_stream stream);
 
 /*
  * Turn-1 causal prefill (Section 3.1: the compute-bound first-turn prefill). For each conversation
@@ -239,7 +326,8 @@ cs_status cs_mixed_step(cs_pool* pool, int32_t n_ext, const cs_conv* ext_convs,
  */
 #define CS_WIRE_FORMAT_VERSION 1
 
-/* Wire size of a conversation's KV: n_layers * ceil(len/16) * n_kv_heads * 64 * head_dim bytes. */
+/* Wire size of a conversation's KV: n_layers * ceil(len/16) * n_kv_heads * 64 * head_dim bytes (a 4-bit
+ * pool: 17 * head_dim, see cs_kv_pack_fp4). */
 cs_status cs_kv_pack_size(const cs_pool* pool, cs_conv conv, size_t* bytes);
 
 /*
@@ -251,6 +339,18 @@ cs_status cs_kv_pack_size(const cs_pool* pool, cs_conv conv, size_t* bytes);
  */
 cs_status cs_kv_pack(const cs_pool* pool, cs_conv conv, void* dst, size_t dst_bytes,
                      cs_stream stream);
+
+/*
+ * The transfer into a 4-bit pool: cs_kv_pack_fp4 gathers a conversation into the wire that such a pool unpacks,
+ * [layer][logical page][kv_head] blocks of CS_KV_FP4, token slots >= length zeros. From a bf16 pool the values
+ * are rounded as an append to a 4-bit pool rounds them, so a prefiller that attends in bf16 sends 3.76 times
+ * fewer bytes and the decoder holds what it would had the same K and V been appended there. (From a 4-bit pool
+ * it is cs_kv_pack.) cs_kv_pack_fp4_size: n_layers * ceil(len/16) * n_kv_heads * 17 * head_dim bytes.
+ * Errors: as cs_kv_pack_size and cs_kv_pack. The format is frozen at CS_WIRE_FP4_VERSION.
+ */
+#define CS_WIRE_FP4_VERSION 1
+cs_status cs_kv_pack_fp4_size(const cs_pool* pool, cs_conv conv, size_t* bytes);
+cs_status cs_kv_pack_fp4(const cs_pool* pool, cs_conv conv, void* dst, size_t dst_bytes, cs_stream stream);
 
 /*
  * Receiving half of the transfer: create a conversation of n_tokens tokens in `pool`, take fresh
@@ -279,6 +379,7 @@ enum {
   CS_PROF_ATTN_FWD = 5,      /* prefill / extend attention kernel and the merge of cut tiles */
   CS_PROF_MIXED_LAYER = 6,   /* one layer's extend tiles + decode split in one launch */
   CS_PROF_KINDS = 7
+  /* queries rotated by cs_rope_q count as CS_PROF_APPEND, cs_kv_read as CS_PROF_UNPACK */
 };
 cs_status cs_profile_start(cs_pool* pool);
 cs_status cs_profile_stop(cs_pool* pool, double* ms, int64_t* launches);

@@ -22,6 +22,10 @@ STATUS_NAMES = {CS_EINVAL: "CS_EINVAL", CS_ENOMEM: "CS_ENOMEM", CS_ENOENT: "CS_E
                 CS_ESTATE: "CS_ESTATE", CS_ERANGE: "CS_ERANGE", CS_EHIP: "CS_EHIP",
                 CS_EBUSY: "CS_EBUSY"}
 PAGE_TOKENS = 16
+CS_KV_BF16, CS_KV_FP4 = 0, 1  # cs_pool_create_as
+KV_FORMATS = {"bf16": CS_KV_BF16, "fp4": CS_KV_FP4}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "parts": 3}   # CS_ROPE_*
+WIRE_FP4_VERSION = 1          # CS_WIRE_FP4_VERSION: the frozen layout of kv_pack_fp4
 WIRE_FORMAT_VERSION = 1       # CS_WIRE_FORMAT_VERSION: the frozen layout of kv_pack / kv_unpack
 
 EXPORTS = [
@@ -29,6 +33,8 @@ EXPORTS = [
     "cs_pool_occupancy", "cs_conv_create", "cs_conv_destroy", "cs_conv_len", "cs_conv_pages",
     "cs_kv_append", "cs_kv_append_batch", "cs_attn_prefill_turn1", "cs_attn_extend",
     "cs_attn_decode_batch", "cs_attn_decode_batch_noalloc", "cs_mixed_step", "cs_kv_pack_size", "cs_kv_pack", "cs_kv_unpack",
+    "cs_pool_kv_bytes_as", "cs_pool_create_as", "cs_rope_init", "cs_kv_append_rope", "cs_rope_q", "cs_kv_read",
+    "cs_kv_pack_fp4_size", "cs_kv_pack_fp4",
     "cs_profile_start",
     "cs_profile_stop", "cs_device_info", "cs_probe_stream_read", "cs_debug_fail_launches",
     "cs_last_error",
@@ -61,6 +67,11 @@ class DeviceInfo(ctypes.Structure):
                 ("l2_bytes", ctypes.c_int64), ("total_mem_bytes", ctypes.c_int64)]
 
 
+class RopeDesc(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("amplitude", ctypes.c_double),
+                ("inv_freq", ctypes.c_double * 64)]
+
+
 class PrefillCurve(ctypes.Structure):
     _fields_ = [("c0", ctypes.c_double), ("c1", ctypes.c_double), ("c2", ctypes.c_double)]
 
@@ -84,6 +95,15 @@ def load_library(path: str = _LIB_PATH) -> ctypes.CDLL:
         "cs_pool_workspace_bytes": (SZ, [ctypes.POINTER(PoolDesc)]),
         "cs_pool_create": (I32, [ctypes.POINTER(PoolDesc), VP, SZ, VP, SZ, ctypes.c_uint64,
                                  ctypes.POINTER(P)]),
+        "cs_pool_kv_bytes_as": (SZ, [ctypes.POINTER(PoolDesc), I32]),
+        "cs_pool_create_as": (I32, [ctypes.POINTER(PoolDesc), I32, VP, SZ, VP, SZ, ctypes.c_uint64,
+                                    ctypes.POINTER(P)]),
+        "cs_rope_init": (I32, [ctypes.POINTER(RopeDesc), I32, I32, ctypes.c_double, I32] + [ctypes.c_double] * 4),
+        "cs_kv_append_rope": (I32, [P, ctypes.POINTER(RopeDesc), I32, VP, VP, VP, VP, VP, VP, VP]),
+        "cs_rope_q": (I32, [P, ctypes.POINTER(RopeDesc), I32, VP, VP, I32, VP, VP, VP]),
+        "cs_kv_read": (I32, [P, I32, VP, VP, VP, VP, VP, VP]),
+        "cs_kv_pack_fp4_size": (I32, [P, I32, ctypes.POINTER(SZ)]),
+        "cs_kv_pack_fp4": (I32, [P, I32, VP, SZ, VP]),
         "cs_pool_destroy": (I32, [P]),
         "cs_pool_occupancy": (I32, [P, PI64, PI64]),
         "cs_conv_create": (I32, [P, PI32]),
@@ -155,34 +175,86 @@ def _aligned_bytes(n: int, device: torch.device, align: int = 256) -> torch.Tens
     return raw[off:off + n]
 
 
+class Rope:
+    """Rotary positions (cs_rope): the first ``rotary_dim`` dims of a head turn with the token's position,
+    pair i = dims (i, i + rotary_dim/2) or, ``interleaved``, (2 i, 2 i + 1), by base^(-2 i / rotary_dim) radians
+    a token. ``scaling`` for contexts ``factor`` times those of training (``original_len`` tokens): "none",
+    "linear", "ntk" or "parts" (pairs of fewer than ``low_turns`` turns over the original context slow down,
+    of more than ``high_turns`` do not); see cs_rope_init. ``amplitude`` and ``inv_freq`` may be set afterwards.
+    """
+
+    def __init__(self, rotary_dim, base=10000.0, interleaved=False, scaling="none", factor=1.0, original_len=0.0,
+                 low_turns=1.0, high_turns=32.0):
+        if scaling not in ROPE_SCALINGS:
+            raise ValueError(f"scaling must be one of {sorted(ROPE_SCALINGS)}, got {scaling!r}")
+        self.desc = RopeDesc()
+        lib = load_library()
+        _check(lib.cs_rope_init(ctypes.byref(self.desc), int(rotary_dim), int(bool(interleaved)), float(base),
+                                ROPE_SCALINGS[scaling], float(factor), float(original_len), float(low_turns),
+                                float(high_turns)))
+
+    @property
+    def rotary_dim(self) -> int:
+        return self.desc.rotary_dim
+
+    @property
+    def interleaved(self) -> bool:
+        return bool(self.desc.interleaved)
+
+    @property
+    def amplitude(self) -> float:
+        return self.desc.amplitude
+
+    @amplitude.setter
+    def amplitude(self, x) -> None:
+        self.desc.amplitude = float(x)
+
+    @property
+    def inv_freq(self) -> np.ndarray:
+        """Radians per position of each pair."""
+        return np.array(self.desc.inv_freq[:self.desc.rotary_dim // 2], dtype=np.float64)
+
+    @inv_freq.setter
+    def inv_freq(self, xs) -> None:
+        xs = np.asarray(xs, dtype=np.float64).reshape(-1)
+        if xs.size != self.desc.rotary_dim // 2:
+            raise ValueError(f"inv_freq must have {self.desc.rotary_dim // 2} values, got {xs.size}")
+        self.desc.inv_freq[:xs.size] = xs.tolist()
+
+
 class KVPool:
     """A pool of 16-token KV pages on one GPU, and the conversations that own them.
 
     Device memory for the pool and its workspace is allocated with torch on ``device``. Method
-    names follow the C ABI (cs_<name>).
+    names follow the C ABI (cs_<name>). ``kv_format``: what the pages hold, "bf16" or "fp4" (4-bit values
+    with power-of-two scales; all calls take and give bf16 either way).
     """
 
     def __init__(self, n_layers, n_q_heads, n_kv_heads, head_dim, n_pages, max_convs,
-                 max_pages_per_conv, placement_seed=0, device="cuda"):
+                 max_pages_per_conv, placement_seed=0, device="cuda", kv_format="bf16"):
+        if kv_format not in KV_FORMATS:
+            raise ValueError(f"kv_format must be one of {sorted(KV_FORMATS)}, got {kv_format!r}")
         self.lib = load_library()
+        self.kv_format = kv_format
+        fmt = KV_FORMATS[kv_format]
         self.desc = PoolDesc(n_layers, n_q_heads, n_kv_heads, head_dim, max_convs,
                              max_pages_per_conv, n_pages)
         self.device = torch.device(device)
         self.n_layers, self.n_q_heads, self.n_kv_heads, self.head_dim = (
             n_layers, n_q_heads, n_kv_heads, head_dim)
-        kvb = self.lib.cs_pool_kv_bytes(ctypes.byref(self.desc))
+        kvb = self.lib.cs_pool_kv_bytes_as(ctypes.byref(self.desc), fmt)
         wsb = self.lib.cs_pool_workspace_bytes(ctypes.byref(self.desc))
         if kvb == 0 or wsb == 0:
             self._handle = None
             # let cs_pool_create report why the descriptor is invalid
             h = ctypes.c_void_p()
-            _check(self.lib.cs_pool_create(ctypes.byref(self.desc), None, 0, None, 0, 0,
-                                           ctypes.byref(h)))
+            _check(self.lib.cs_pool_create_as(ctypes.byref(self.desc), fmt, None, 0, None, 0, 0,
+                                              ctypes.byref(h)))
         self.kv = _aligned_bytes(kvb, self.device)
         self.ws = _aligned_bytes(wsb, self.device)
         h = ctypes.c_void_p()
-        _check(self.lib.cs_pool_create(ctypes.byref(self.desc), self.kv.data_ptr(), kvb,
-                                       self.ws.data_ptr(), wsb, placement_seed, ctypes.byref(h)))
+        _check(self.lib.cs_pool_create_as(ctypes.byref(self.desc), fmt, self.kv.data_ptr(), kvb,
+                                          self.ws.data_ptr(), wsb, placement_seed, ctypes.byref(h)))
         self._handle = h
 
     # -- lifetime ------------------------------------------------------------------------------
@@ -205,11 +277,14 @@ class KVPool:
 
     @property
     def page_block_bytes(self) -> int:
-        return 2 * PAGE_TOKENS * self.head_dim * 2
+        return (17 if self.kv_format == "fp4" else 2 * PAGE_TOKENS * 2) * self.head_dim
 
     def kv_view(self) -> torch.Tensor:
         """The pool as [n_layers][n_pages][n_kv_heads][2*16*head_dim] bf16 bits (int16 view); each
-        block is the K part (head_dim/32 sub-blocks [16 tokens][32 dims]) then V^T[head_dim][16]."""
+        block is the K part (head_dim/32 sub-blocks [16 tokens][32 dims]) then V^T[head_dim][16].
+        An fp4 pool: [n_layers][n_pages][n_kv_heads][17*head_dim] bytes."""
+        if self.kv_format == "fp4":
+            return self.kv.view(self.n_layers, self.desc.n_pages, self.n_kv_heads, self.page_block_bytes)
         return self.kv.view(torch.int16).view(self.n_layers, self.desc.n_pages, self.n_kv_heads,
                                               2 * PAGE_TOKENS * self.head_dim)
 
@@ -273,6 +348,71 @@ class KVPool:
         kp, vp = self._dev(k, "k", shp), self._dev(v, "v", shp)
         _check(self.lib.cs_kv_append_batch(self._handle, len(ca), cp, npp, kp, vp,
                                            _stream_handle(self.device)))
+
+    def kv_append_rope(self, convs, n_new, k: torch.Tensor, v: torch.Tensor, rope: Rope, q: torch.Tensor | None = None,
+                       q_out: torch.Tensor | None = None):
+        """kv_append_batch with the keys rotated at their positions. With q, the queries of the same tokens
+        [n_layers][sum(n_new)][n_q_heads][head_dim], those are rotated too, into q_out (new if None; q itself
+        rotates in place); returns q_out."""
+        ca, cp = _i32_array(convs)
+        na, npp = _i32_array(n_new)
+        if len(ca) != len(na):
+            raise ValueError("convs and n_new differ in length")
+        shp = (self.n_layers, sum(na), self.n_kv_heads, self.head_dim)
+        kp, vp = self._dev(k, "k", shp), self._dev(v, "v", shp)
+        qp = op = None
+        if q is not None:
+            qshp = (self.n_layers, sum(na), self.n_q_heads, self.head_dim)
+            qp = self._dev(q, "q", qshp)
+            if q_out is None:
+                q_out = torch.empty(qshp, dtype=torch.bfloat16, device=self.device)
+            op = self._rotated(q, q_out, "q_out", qshp)
+        elif q_out is not None:
+            raise ValueError("q_out without q")
+        _check(self.lib.cs_kv_append_rope(self._handle, ctypes.byref(rope.desc), len(ca), cp, npp, kp, vp, qp, op,
+                                          _stream_handle(self.device)))
+        return q_out
+
+    def rope_q(self, convs, q_lens, q: torch.Tensor, rope: Rope, out: torch.Tensor | None = None) -> torch.Tensor:
+        """Queries of the last q_lens[i] positions of each conversation, rotated: q [rows][n_q_heads][head_dim]
+        or [any layers][rows][n_q_heads][head_dim]; out may be q itself."""
+        ca, cp = _i32_array(convs)
+        qa, qlp = _i32_array(q_lens)
+        if len(ca) != len(qa):
+            raise ValueError("convs and q_lens differ in length")
+        shp = (sum(qa), self.n_q_heads, self.head_dim)
+        if q.dim() == 4:
+            shp = (q.shape[0],) + shp
+        qp = self._dev(q, "q", shp)
+        if out is None:
+            out = torch.empty(shp, dtype=torch.bfloat16, device=self.device)
+        op = self._rotated(q, out, "out", shp)
+        _check(self.lib.cs_rope_q(self._handle, ctypes.byref(rope.desc), len(ca), cp, qlp, shp[0] if len(shp) == 4 else 1, qp, op,
+                                  _stream_handle(self.device)))
+        return out
+
+    def _rotated(self, q, out, name, shape) -> int:
+        """The pointer of a rotation's output, which is q itself or does not overlap it."""
+        p, src, n = self._dev(out, name, shape), q.data_ptr(), q.numel() * 2
+        if p != src and p < src + n and src < p + n:
+            raise ValueError(f"{name} overlaps q without being q")
+        return p
+
+    def kv_read(self, convs, starts, lens, k: torch.Tensor | None = None, v: torch.Tensor | None = None):
+        """Tokens starts[i] .. starts[i] + lens[i] - 1 of each conversation back from the cache: (k, v), both
+        [n_layers][sum(lens)][n_kv_heads][head_dim] bf16."""
+        ca, cp = _i32_array(convs)
+        na, npp = _i32_array(lens)
+        sa = array.array("q", [int(x) for x in starts])
+        if not len(ca) == len(na) == len(sa):
+            raise ValueError("convs, starts and lens differ in length")
+        shp = (self.n_layers, sum(na), self.n_kv_heads, self.head_dim)
+        if min(na, default=0) < 0:
+            raise ValueError("lens must not be negative")
+        k, v = (torch.empty(shp, dtype=torch.bfloat16, device=self.device) if x is None else x for x in (k, v))
+        kp, vp = self._dev(k, "k", shp), self._dev(v, "v", shp)
+        _check(self.lib.cs_kv_read(self._handle, len(ca), cp, sa.buffer_info()[0], npp, kp, vp, _stream_handle(self.device)))
+        return k, v
 
     # -- attention -----------------------------------------------------------------------------
     def _attend(self, fn, convs, q_lens, layer, q, out):
@@ -366,13 +506,23 @@ class KVPool:
         return n.value
 
     def kv_pack(self, conv: int, dst: torch.Tensor | None = None) -> torch.Tensor:
-        nbytes = self.kv_pack_size(conv)
+        return self._pack(self.lib.cs_kv_pack, conv, self.kv_pack_size(conv), dst)
+
+    def kv_pack_fp4_size(self, conv: int) -> int:
+        n = ctypes.c_size_t()
+        _check(self.lib.cs_kv_pack_fp4_size(self._handle, conv, ctypes.byref(n)))
+        return n.value
+
+    def kv_pack_fp4(self, conv: int, dst: torch.Tensor | None = None) -> torch.Tensor:
+        """The conversation as the wire of an fp4 pool (rounded to 4 bits, if this pool is bf16)."""
+        return self._pack(self.lib.cs_kv_pack_fp4, conv, self.kv_pack_fp4_size(conv), dst)
+
+    def _pack(self, fn, conv, nbytes, dst) -> torch.Tensor:
         if dst is None:
             dst = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         if not dst.is_contiguous() or dst.device.type != self.device.type:
             raise ValueError("dst must be a contiguous tensor on the pool's device")
-        _check(self.lib.cs_kv_pack(self._handle, conv, dst.data_ptr(),
-                                   dst.numel() * dst.element_size(), _stream_handle(self.device)))
+        _check(fn(self._handle, conv, dst.data_ptr(), dst.numel() * dst.element_size(), _stream_handle(self.device)))
         return dst
 
     def kv_unpack(self, src: torch.Tensor, n_tokens: int) -> int:

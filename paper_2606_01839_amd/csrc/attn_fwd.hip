@@ -39,6 +39,7 @@
 
 #include "decode_split.hpp"
 #include "device_common.hpp"
+#include "fp4.hpp"
 #include "kernels.hpp"
 
 namespace cs {
@@ -114,6 +115,12 @@ __device__ __forceinline__ void dma_wait_barrier() {
   else asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"(N) : "memory");
 }
 
+// The same for tiles that are written to LDS: the wave's LDS operations are complete (lds_wait), then every
+// wave has arrived (bare_barrier).
+__device__ __forceinline__ void lds_wait() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void bare_barrier() { asm volatile("s_barrier" ::: "memory"); }
+__device__ __forceinline__ void lds_wait_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 // One (tile or piece, kv head) workgroup (`block` = its index in the layer's grid, `dl` = its layer
 // counted from a.layer).
 //
@@ -122,7 +129,11 @@ __device__ __forceinline__ void dma_wait_barrier() {
 // Without it a head_dim 64 wave needs 121 registers and two workgroups fit a CU.
 // CHAIN: tiles may hold pieces to take one after the other (a form of its own, since the code around
 // the loop costs launches without such tiles 1.5%).
-template <int D, int G, bool PRE, bool CHAIN>
+//
+// FP4: the pool's blocks hold 4-bit codes (fp4.hpp). They pass through registers instead of the copies above: a
+// wave loads half of a page's K and V codes and their scales a step ahead, converts them at the start of the
+// next and writes them to the ring as the bf16 tile that the other form copies; everything else is the same.
+template <int D, int G, bool PRE, bool CHAIN, bool FP4 = false>
 __device__ __forceinline__ void attn_fwd_block(const ExtendArgs& a, const int block, const int dl) {
   constexpr int NW = 8;                   // waves: G query heads x (8 / G) blocks of 32 queries
   constexpr int BM = 32 * (NW / G);       // queries per workgroup
@@ -189,6 +200,53 @@ __device__ __forceinline__ void attn_fwd_block(const ExtendArgs& a, const int bl
   // conversation's end are its last page), so every step issues the same number and the counter
   // waits below stay exact. Those keys are masked by the causal mask.
   auto page_of = [&](int j) { return ptc[min(4 * min(j, n_kt - 1) + q_w, n_pg - 1)]; };
+  // 4-bit pages: this wave's half of a page (its dims' half of each lane's words) and where it goes.
+  using B4 = Fp4Block<D>;
+  constexpr int NH = B4::kWords / 2;      // words of K, and of V, a lane takes
+  struct Codes {
+    uint32_t k[NH], v[NH], ks, vs;
+  };
+  const int f_c = lane & 15, f_qd = lane >> 4, f_h = wave & 1;
+  const uint8_t* f_base = reinterpret_cast<const uint8_t*>(a.pool) +
+                          (static_cast<size_t>(a.layer + dl) * a.n_pages * a.n_kv_heads + g) * B4::kBytes;
+  const size_t f_stride = static_cast<size_t>(a.n_kv_heads) * B4::kBytes;
+  auto load_codes = [&](int page) {
+    Codes x;
+    const uint8_t* blk = f_base + static_cast<size_t>(page) * f_stride;
+    const uint8_t* kc = blk + B4::kK + (lane * B4::kWords + f_h * NH) * 4;
+    const uint8_t* vc = blk + B4::kV + (lane * B4::kWords + f_h * NH) * 4;
+    if constexpr (NH == 2) {
+      const uint2 kk = ld8(kc), vv = ld8(vc);
+      x.k[0] = kk.x, x.k[1] = kk.y, x.v[0] = vv.x, x.v[1] = vv.y;
+    } else {
+      x.k[0] = *reinterpret_cast<const uint32_t*>(kc);
+      x.v[0] = *reinterpret_cast<const uint32_t*>(vc);
+    }
+    x.ks = blk[B4::k_scale(f_qd, f_c)];
+    x.vs = *reinterpret_cast<const uint32_t*>(blk + B4::kVScale + 4 * f_qd);
+    return x;
+  };
+  // K row of key f_c (bits 2 and 3 swapped, as above), chunks (D / 32) f_qd + NH f_h + i; V^T dims
+  // 16 (2 NH f_h + t) + f_c, keys 4 f_qd .. + 3.
+  const int f_row = (f_c & 3) | ((f_c >> 3) & 1) << 2 | ((f_c >> 2) & 1) << 3;
+  const uint32_t f_krow = static_cast<uint32_t>((kPageTokens * q_w + f_row) * (2 * D));
+  const uint32_t f_v = static_cast<uint32_t>(q_w * (kPageTokens * 2 * D) + (32 * NH * f_h + f_c) * 32 +
+                                             (((f_qd >> 1) ^ ((f_c >> 2) & 1) ^ ((f_c >> 3) & 1)) * 16) + (f_qd & 1) * 8);
+  auto store_codes = [&](const Codes& x, int buf) {
+    const float ks = fp4_scale(x.ks);
+#pragma unroll
+    for (int i = 0; i < NH; ++i) {
+      const int chunk = (B4::kWords * f_qd + NH * f_h + i) ^ swz(f_row);
+      st16(smem + buf * HALF_TILE + f_krow + chunk * 16, fp4_word(x.k[i], ks));
+    }
+    const float vs[4] = {fp4_scale_of(x.vs, 0), fp4_scale_of(x.vs, 1), fp4_scale_of(x.vs, 2), fp4_scale_of(x.vs, 3)};
+#pragma unroll
+    for (int i = 0; i < NH; ++i) {   // (16 dims on: 512 bytes; bits 2 and 3 of the dim are f_c's)
+      st8(smem + VBASE + buf * HALF_TILE + f_v + (2 * i) * 512, fp4_quad<0>(x.v[i], vs));
+      st8(smem + VBASE + buf * HALF_TILE + f_v + (2 * i + 1) * 512, fp4_quad<1>(x.v[i], vs));
+    }
+  };
+  Codes codes{};   // of the tile after the next
   auto copy_tile = [&](int page, int buf) {
     const uint16_t* blk = a.pool + layer_base + static_cast<size_t>(page) * page_stride;
 #pragma unroll
@@ -223,8 +281,15 @@ __device__ __forceinline__ void attn_fwd_block(const ExtendArgs& a, const int bl
   for (int ks = 0; ks < KS; ++ks) qop[ks] = as_bf16x8(ld16(qrow + 16 * ks + 8 * half));  // padding rows: row 0
   // (one vector load of the first four tiles' pages: one trip to memory instead of four)
   const int pages = pt[min(4 * min(kt0 + (lane & 3), n_kt - 1) + q_w, n_pg - 1)];
+  Codes first[2];
+  if constexpr (FP4) {
+    first[0] = load_codes(__builtin_amdgcn_readlane(pages, 0));
+    first[1] = load_codes(__builtin_amdgcn_readlane(pages, 1));
+    codes = load_codes(__builtin_amdgcn_readlane(pages, 2));
+  } else {
 #pragma unroll
-  for (int i = 0; i < 3; ++i) copy_tile(__builtin_amdgcn_readlane(pages, i), i);
+    for (int i = 0; i < 3; ++i) copy_tile(__builtin_amdgcn_readlane(pages, i), i);
+  }
   int page_next = __builtin_amdgcn_readlane(pages, 3);
   __builtin_amdgcn_sched_barrier(0);   // no wait for Q before the copies are issued
   // Q must have arrived before the loop: a wait of the compiler's at the loop head would drain the copies
@@ -246,14 +311,30 @@ __device__ __forceinline__ void attn_fwd_block(const ExtendArgs& a, const int bl
   float m_s = -FLT_MAX, l_run = 0.f;
   const bf16x2 ones = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
 
-  dma_wait_barrier<2 * BPW>();   // tiles 0 and 1 landed
+  // Start of a step: the tile three (4-bit pages: two) ahead goes on its way into the ring.
+  auto feed = [&](int buf) {
+    if constexpr (FP4) {
+      store_codes(codes, (buf + 2) % NBUF);
+      codes = load_codes(page_next);
+    } else {
+      copy_tile(page_next, (buf + 3) % NBUF);
+    }
+  };
+  if constexpr (FP4) {
+    store_codes(first[0], 0);
+    store_codes(first[1], 1);
+    lds_wait_barrier();
+  } else {
+    dma_wait_barrier<2 * BPW>();   // tiles 0 and 1 landed
+  }
   if (qrow0 >= cd.q_len) {
     // A wave whose 32 query rows all lie past the chunk's end only does its share of the copies and
     // leaves the matrix cores to the others (17 tokens on 1007 at G = 4: 29.2 -> 19.6 us).
     for (int j = kt0; j < n_kt; ++j) {
-      copy_tile(page_next, (j - kt0 + 3) % NBUF);
+      feed((j - kt0) % NBUF);
       page_next = page_of(j + 4);
-      dma_wait_barrier<2 * BPW>();
+      if constexpr (FP4) lds_wait_barrier();
+      else dma_wait_barrier<2 * BPW>();
     }
     dma_wait_barrier<0>();
     return;
@@ -275,7 +356,7 @@ __device__ __forceinline__ void attn_fwd_block(const ExtendArgs& a, const int bl
   if constexpr (PRE) read_k(0);
 
   auto tile_step = [&](const int j, const int buf) {
-    copy_tile(page_next, (buf + 3) % NBUF);
+    feed(buf);
     f32x16 s[2];
 #pragma unroll
     for (int kt2 = 0; kt2 < 2; ++kt2)
@@ -360,12 +441,16 @@ __device__ __forceinline__ void attn_fwd_block(const ExtendArgs& a, const int bl
         for (int t = 0; t < DT; ++t)
           o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(PRE ? vop[kt2][j2][t] : v_operand(buf, kt2, j2, t),
                                                          pop[kt2][j2], o[t], 0, 0, 0);
+    // 4-bit pages: the wave's writes of tile j+2 (and its V^T reads) are complete before the barrier; the K
+    // reads below may be in flight there.
+    if constexpr (FP4) lds_wait();
     if constexpr (PRE) read_k((buf + 1) % NBUF);      // tile j+1 is in LDS (waited at the end of step j-1)
     // this wave's copies of tile j+2 have landed (those of tile j+3 may still fly); after the
     // barrier every wave's have. The next step copies over this step's buffer. With PRE its V^T operands
     // were read before the softmax and the reads still in flight are the next tile's K, a buffer that is
     // copied over a step later; without PRE the last V^T reads are waited for here.
-    dma_wait_barrier<2 * BPW, !PRE>();
+    if constexpr (FP4) bare_barrier();
+    else dma_wait_barrier<2 * BPW, !PRE>();
   };
   // One piece's record: the accumulators as they lie in the registers (every store 1 KiB of consecutive
   // bytes per wave), then (maximum, sum) of each lane's row.
@@ -550,6 +635,13 @@ void attn_fwd_kernel(LaunchMeta, ExtendArgs a) {
   attn_fwd_block<D, G, PRE, CHAIN>(a, blockIdx.x, blockIdx.y);
 }
 
+// the same over 4-bit pages
+template <int D, int G, bool PRE, bool CHAIN>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(PRE ? 2 : 4)))
+void attn_fp4_kernel(LaunchMeta, ExtendArgs a) {
+  attn_fwd_block<D, G, PRE, CHAIN, true>(a, blockIdx.x, blockIdx.y);
+}
+
 template <int D, int G>
 __global__ __launch_bounds__(256) void extend_merge_kernel(LaunchMeta, ExtendArgs a) {
   extend_merge_body<D, G>(a, blockIdx.x, blockIdx.y, threadIdx.x);
@@ -563,19 +655,32 @@ __global__ __launch_bounds__(256) void extend_merge_kernel(LaunchMeta, ExtendArg
 // Units of n_kv_heads workgroups are taken in an order that spreads the extend units evenly over the
 // first n_mix units, so that at any time some CUs use the matrix cores while others read HBM; n_mix =
 // their number puts them all in front (tiles longer than everything else).
-template <int D, int G, bool CHAIN>
-__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2)))
-void mixed_layer_kernel(ExtendArgs ea, int n_ext, int n_mix, DecodeArgs da) {
+template <int D, int G, bool CHAIN, bool FP4>
+__device__ __forceinline__ void mixed_layer_block(const ExtendArgs& ea, int n_ext, int n_mix, const DecodeArgs& da, float* xch) {
   static_assert(kDecodeItemThreads == 512, "a decode work item fills one attention workgroup");
-  __shared__ float xch[split_exchange_floats<D>()];
   const int unit = blockIdx.x / ea.n_kv_heads, head = blockIdx.x % ea.n_kv_heads;
   const int before = unit < n_mix ? static_cast<int>(static_cast<int64_t>(unit) * n_ext / n_mix) : n_ext;
   const int after = unit < n_mix ? static_cast<int>(static_cast<int64_t>(unit + 1) * n_ext / n_mix) : n_ext;
   if (after > before) {
-    attn_fwd_block<D, G, true, CHAIN>(ea, before * ea.n_kv_heads + head, 0);
+    attn_fwd_block<D, G, true, CHAIN, FP4>(ea, before * ea.n_kv_heads + head, 0);
     return;
   }
-  split_body<D>(da, (unit - before) * ea.n_kv_heads + head, 0, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), xch);
+  split_body<D, FP4>(da, (unit - before) * ea.n_kv_heads + head, 0, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), xch);
+}
+
+template <int D, int G, bool CHAIN>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2)))
+void mixed_layer_kernel(ExtendArgs ea, int n_ext, int n_mix, DecodeArgs da) {
+  __shared__ float xch[split_exchange_floats<D>()];
+  mixed_layer_block<D, G, CHAIN, false>(ea, n_ext, n_mix, da, xch);
+}
+
+// the same over 4-bit pages
+template <int D, int G, bool CHAIN>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2)))
+void mixed_fp4_kernel(ExtendArgs ea, int n_ext, int n_mix, DecodeArgs da) {
+  __shared__ float xch[split_exchange_floats<D>()];
+  mixed_layer_block<D, G, CHAIN, true>(ea, n_ext, n_mix, da, xch);
 }
 
 // What is left of that layer: the first n_ext workgroups merge its cut extend tiles, the others its
@@ -649,6 +754,13 @@ hipError_t launch_extend(const PoolGeom& g, int layer, int n_layers, const Exten
     return hipGetLastError();
   };
   return by_shape(g, [&](auto d, auto grp) {
+    if (g.fp4) {
+      if constexpr (d() == 64) {
+        if (two_per_cu)
+          return e.chained ? launch(attn_fp4_kernel<d(), grp(), false, true>) : launch(attn_fp4_kernel<d(), grp(), false, false>);
+      }
+      return e.chained ? launch(attn_fp4_kernel<d(), grp(), true, true>) : launch(attn_fp4_kernel<d(), grp(), true, false>);
+    }
     if constexpr (d() == 64) {
       if (two_per_cu)
         return e.chained ? launch(attn_fwd_kernel<d(), grp(), false, true>) : launch(attn_fwd_kernel<d(), grp(), false, false>);
@@ -687,7 +799,9 @@ hipError_t launch_mixed_layer(const PoolGeom& g, int layer, const ExtendLaunch& 
   const int n_mix = e.n_tiles + (e.n_merges > 0 ? w.n_items * 6 / 10 : 0);
   const int blocks = (e.n_tiles + w.n_items) * g.n_kv_heads;
   return by_shape(g, [&](auto d, auto grp) {
-    if (e.chained) mixed_layer_kernel<d(), grp(), true><<<blocks, 512, 0, stream>>>(ea, e.n_tiles, n_mix, da);
+    if (g.fp4 && e.chained) mixed_fp4_kernel<d(), grp(), true><<<blocks, 512, 0, stream>>>(ea, e.n_tiles, n_mix, da);
+    else if (g.fp4) mixed_fp4_kernel<d(), grp(), false><<<blocks, 512, 0, stream>>>(ea, e.n_tiles, n_mix, da);
+    else if (e.chained) mixed_layer_kernel<d(), grp(), true><<<blocks, 512, 0, stream>>>(ea, e.n_tiles, n_mix, da);
     else mixed_layer_kernel<d(), grp(), false><<<blocks, 512, 0, stream>>>(ea, e.n_tiles, n_mix, da);
     return hipGetLastError();
   });

@@ -95,6 +95,7 @@ const char* desc_problem(const cs_pool_desc* d) {
 
 struct cs_pool {
   cs_pool_desc desc;
+  bool fp4;   // CS_KV_FP4
   char* kv;
   size_t kv_bytes;
   char* ws;
@@ -135,8 +136,8 @@ struct cs_pool {
   std::vector<hipEvent_t> ev_free;
   std::vector<ProfEvent> prof_events;
 
-  cs_pool(const cs_pool_desc& d, char* kvp, size_t kvb, char* wsp, size_t wsb, uint64_t seed)
-      : desc(d), kv(kvp), kv_bytes(kvb), ws(wsp), ws_bytes(wsb), lay(ws_layout(d)),
+  cs_pool(const cs_pool_desc& d, bool fp4_pages, char* kvp, size_t kvb, char* wsp, size_t wsb, uint64_t seed)
+      : desc(d), fp4(fp4_pages), kv(kvp), kv_bytes(kvb), ws(wsp), ws_bytes(wsb), lay(ws_layout(d)),
         pages(d.n_pages, seed), convs(d.max_convs, d.max_pages_per_conv) {}
 
   cs::PoolGeom geom() const {
@@ -149,6 +150,7 @@ struct cs_pool {
     g.head_dim = desc.head_dim;
     g.page_table = reinterpret_cast<int32_t*>(ws + lay.page_table);
     g.max_pages = desc.max_pages_per_conv;
+    g.fp4 = fp4;
     return g;
   }
   float* partials() const { return reinterpret_cast<float*>(ws + lay.partials); }
@@ -393,9 +395,38 @@ cs_status check_convs(cs_pool* p, int32_t n, const cs_conv* convs, std::vector<c
   return CS_OK;
 }
 
-size_t wire_size(const cs_pool_desc& d, int64_t len) {
+// Bytes of a block (page, kv head) of one layer: K and V of 16 tokens, in bf16 or in 4 bits with scales.
+size_t block_bytes(const cs_pool_desc& d, bool fp4) {
+  return static_cast<size_t>(d.head_dim) * (fp4 ? 17 : 2 * cs::kPage * 2);
+}
+
+size_t wire_size(const cs_pool_desc& d, bool fp4, int64_t len) {
   return static_cast<size_t>(d.n_layers) * static_cast<size_t>(cs::pages_for(len)) *
-         static_cast<size_t>(d.n_kv_heads) * 2 * cs::kPage * static_cast<size_t>(d.head_dim) * 2;
+         static_cast<size_t>(d.n_kv_heads) * block_bytes(d, fp4);
+}
+
+// A rotation as the kernels take it: each pair's turns per position as a 64-bit fraction of a turn (whole
+// turns drop out, positions being whole numbers).
+cs_status rope_args(const cs_pool_desc& d, const cs_rope* r, cs::RopeArgs* out) {
+  if (!r) return fail(CS_EINVAL, "null rope");
+  if (r->rotary_dim < 16 || r->rotary_dim % 16 != 0 || r->rotary_dim > d.head_dim)
+    return fail(CS_EINVAL, "rotary_dim must be a multiple of 16 in 16 .. head_dim");
+  if (r->interleaved != 0 && r->interleaved != 1) return fail(CS_EINVAL, "interleaved must be 0 or 1");
+  if (!std::isfinite(r->amplitude)) return fail(CS_EINVAL, "the rotation's amplitude is not finite");
+  *out = cs::RopeArgs{};
+  out->pairs = r->rotary_dim / 2;
+  out->interleaved = r->interleaved;
+  out->amplitude = static_cast<float>(r->amplitude);
+  if (!std::isfinite(out->amplitude)) return fail(CS_EINVAL, "the rotation's amplitude is not finite");
+  constexpr long double kTwoPi = 6.283185307179586476925286766559005768L;
+  for (int i = 0; i < out->pairs; ++i) {
+    if (!std::isfinite(r->inv_freq[i])) return fail(CS_EINVAL, "a rotation frequency is not finite");
+    long double turns = std::fmod(static_cast<long double>(r->inv_freq[i]) / kTwoPi, 1.0L);
+    if (turns < 0) turns += 1.0L;
+    const long double f = std::floor(turns * 18446744073709551616.0L + 0.5L);   // may round up to a whole turn
+    out->frac[i] = f >= 18446744073709551616.0L ? 0 : static_cast<uint64_t>(f);
+  }
+  return CS_OK;
 }
 
 hipStream_t as_stream(cs_stream s) { return reinterpret_cast<hipStream_t>(s); }
@@ -613,9 +644,16 @@ cs_status check_append(const cs_pool* p, const std::vector<const cs::Conv*>& cv,
 
 // `carry` (may be null): metadata of the launches that follow the append in the same call; on success
 // *carry_dev is its device address.
+struct RotatedAppend {
+  cs::RopeArgs rope;
+  const void* q = nullptr;   // may be null
+  void* q_out = nullptr;
+};
+
+// `rotated` (may be null): keys turn on their way into the pages, and the queries with them.
 cs_status append_impl(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t* n_new,
                       const void* k, const void* v, cs_stream stream, const Blob* carry = nullptr,
-                      void** carry_dev = nullptr) {
+                      void** carry_dev = nullptr, const RotatedAppend* rotated = nullptr) {
   if (!p) return fail(CS_EINVAL, "null pool");
   std::vector<const cs::Conv*> cv;
   cs_status st = check_convs(p, n, convs, cv);
@@ -658,8 +696,12 @@ cs_status append_impl(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t
   const cs::PoolGeom g = p->geom();
   const size_t carry_bytes = carry ? carry->bytes.size() : 0;
   auto launch = [&](const cs::Meta& m, int n_chunks, const cs::AppendCarry& c) {
-    return timed_launch(p, CS_PROF_APPEND, "append launch",
-                        [&] { return cs::launch_append(g, m, n_chunks, c, k, v, total, p->stream); });
+    return timed_launch(p, CS_PROF_APPEND, "append launch", [&] {
+      if (rotated)
+        return cs::launch_append_as(g, m, n_chunks, c, &rotated->rope, k, v, rotated->q, rotated->q_out, total, p->stream);
+      if (p->fp4) return cs::launch_append_as(g, m, n_chunks, c, nullptr, k, v, nullptr, nullptr, total, p->stream);
+      return cs::launch_append(g, m, n_chunks, c, k, v, total, p->stream);
+    });
   };
   if (chunks.size() * sizeof(cs::PageChunk) + carry_bytes <= cs::kMetaBytes) {
     // small: the chunks travel in the launch's arguments, and so does the metadata of the launches
@@ -706,11 +748,13 @@ extern "C" {
 
 const char* cs_last_error(void) { return g_err.c_str(); }
 
-size_t cs_pool_kv_bytes(const cs_pool_desc* d) {
-  if (desc_problem(d)) return 0;
+size_t cs_pool_kv_bytes_as(const cs_pool_desc* d, int32_t format) {
+  if (desc_problem(d) || (format != CS_KV_BF16 && format != CS_KV_FP4)) return 0;
   return static_cast<size_t>(d->n_layers) * static_cast<size_t>(d->n_pages) *
-         static_cast<size_t>(d->n_kv_heads) * 2 * cs::kPage * static_cast<size_t>(d->head_dim) * 2;
+         static_cast<size_t>(d->n_kv_heads) * block_bytes(*d, format == CS_KV_FP4);
 }
+
+size_t cs_pool_kv_bytes(const cs_pool_desc* d) { return cs_pool_kv_bytes_as(d, CS_KV_BF16); }
 
 size_t cs_pool_workspace_bytes(const cs_pool_desc* d) {
   if (desc_problem(d)) return 0;
@@ -719,16 +763,22 @@ size_t cs_pool_workspace_bytes(const cs_pool_desc* d) {
 
 cs_status cs_pool_create(const cs_pool_desc* d, void* kv_base, size_t kv_bytes, void* ws_base,
                          size_t ws_bytes, uint64_t seed, cs_pool** out) {
+  return cs_pool_create_as(d, CS_KV_BF16, kv_base, kv_bytes, ws_base, ws_bytes, seed, out);
+}
+
+cs_status cs_pool_create_as(const cs_pool_desc* d, int32_t format, void* kv_base, size_t kv_bytes, void* ws_base,
+                            size_t ws_bytes, uint64_t seed, cs_pool** out) {
   if (const char* why = desc_problem(d)) return fail(CS_EINVAL, why);
+  if (format != CS_KV_BF16 && format != CS_KV_FP4) return fail(CS_EINVAL, "unknown KV format");
   if (!out) return fail(CS_EINVAL, "null out");
   if (!kv_base || !ws_base) return fail(CS_EINVAL, "null kv or workspace base");
   if (reinterpret_cast<uintptr_t>(kv_base) % kAlign || reinterpret_cast<uintptr_t>(ws_base) % kAlign)
     return fail(CS_EINVAL, "kv and workspace bases must be 256-byte aligned");
-  if (kv_bytes < cs_pool_kv_bytes(d)) return fail(CS_EINVAL, "kv buffer smaller than cs_pool_kv_bytes");
+  if (kv_bytes < cs_pool_kv_bytes_as(d, format)) return fail(CS_EINVAL, "kv buffer smaller than cs_pool_kv_bytes");
   if (ws_bytes < cs_pool_workspace_bytes(d))
     return fail(CS_EINVAL, "workspace smaller than cs_pool_workspace_bytes");
   cs_pool* p = new (std::nothrow)
-      cs_pool(*d, static_cast<char*>(kv_base), kv_bytes, static_cast<char*>(ws_base), ws_bytes, seed);
+      cs_pool(*d, format == CS_KV_FP4, static_cast<char*>(kv_base), kv_bytes, static_cast<char*>(ws_base), ws_bytes, seed);
   if (!p) return fail(CS_ENOMEM, "host allocation failed");
   *out = p;
   return CS_OK;
@@ -807,6 +857,130 @@ cs_status cs_kv_append(cs_pool* p, cs_conv conv, int32_t n_new, const void* k, c
 cs_status cs_kv_append_batch(cs_pool* p, int32_t n_convs, const cs_conv* convs, const int32_t* n_new,
                              const void* k, const void* v, cs_stream stream) {
   return append_impl(p, n_convs, convs, n_new, k, v, stream);
+}
+
+cs_status cs_rope_init(cs_rope* out, int32_t rotary_dim, int32_t interleaved, double base, int32_t scaling, double factor,
+                       double original_len, double low_turns, double high_turns) {
+  if (!out) return fail(CS_EINVAL, "null out");
+  if (rotary_dim < 16 || rotary_dim > 128 || rotary_dim % 16) return fail(CS_EINVAL, "rotary_dim must be a multiple of 16 in 16 .. 128");
+  if (interleaved != 0 && interleaved != 1) return fail(CS_EINVAL, "interleaved must be 0 or 1");
+  if (!(base > 1) || !std::isfinite(base)) return fail(CS_EINVAL, "base must be greater than 1");
+  if (scaling < CS_ROPE_PLAIN || scaling > CS_ROPE_PARTS) return fail(CS_EINVAL, "unknown scaling");
+  if (scaling != CS_ROPE_PLAIN && (!(factor >= 1) || !std::isfinite(factor))) return fail(CS_EINVAL, "factor must be at least 1");
+  if (scaling == CS_ROPE_PARTS && (!(original_len > 0) || !std::isfinite(original_len) || !std::isfinite(low_turns) ||
+                                   !std::isfinite(high_turns) || !(low_turns < high_turns)))
+    return fail(CS_EINVAL, "original_len must be positive and low_turns less than high_turns");
+  cs_rope r{};
+  r.rotary_dim = rotary_dim;
+  r.interleaved = interleaved;
+  r.amplitude = scaling == CS_ROPE_PARTS ? 0.1 * std::log(factor) + 1.0 : 1.0;
+  if (scaling == CS_ROPE_NTK) base *= std::pow(factor, rotary_dim / (rotary_dim - 2.0));
+  for (int i = 0; i < rotary_dim / 2; ++i) {
+    double f = std::pow(base, -2.0 * i / rotary_dim);
+    if (scaling == CS_ROPE_LINEAR) f /= factor;
+    if (scaling == CS_ROPE_PARTS) {
+      const double turns = original_len * f / 6.283185307179586;
+      const double g = std::min(1.0, std::max(0.0, (turns - low_turns) / (high_turns - low_turns)));
+      f *= g + (1 - g) / factor;
+    }
+    r.inv_freq[i] = f;
+  }
+  *out = r;
+  return CS_OK;
+}
+
+cs_status cs_kv_append_rope(cs_pool* p, const cs_rope* rope, int32_t n_convs, const cs_conv* convs, const int32_t* n_new,
+                            const void* k, const void* v, const void* q, void* q_out, cs_stream stream) {
+  if (!p) return fail(CS_EINVAL, "null pool");
+  RotatedAppend r;
+  const cs_status st = rope_args(p->desc, rope, &r.rope);
+  if (st != CS_OK) return st;
+  if (q && !q_out) return fail(CS_EINVAL, "null q_out");
+  r.q = q;
+  r.q_out = q_out;
+  return append_impl(p, n_convs, convs, n_new, k, v, stream, nullptr, nullptr, &r);
+}
+
+cs_status cs_rope_q(cs_pool* p, const cs_rope* rope, int32_t n, const cs_conv* convs, const int32_t* q_lens, int32_t n_layers,
+                    const void* q, void* out, cs_stream stream) {
+  if (!p) return fail(CS_EINVAL, "null pool");
+  cs::RopeArgs r;
+  cs_status st = rope_args(p->desc, rope, &r);
+  if (st != CS_OK) return st;
+  std::vector<const cs::Conv*> cv;
+  if ((st = check_convs(p, n, convs, cv)) != CS_OK) return st;
+  if (n > 0 && !q_lens) return fail(CS_EINVAL, "null q_lens");
+  if (n_layers < 0) return fail(CS_EINVAL, "negative layer count");
+  int64_t rows = 0;
+  std::vector<cs::RopeConv> rc;
+  rc.reserve(static_cast<size_t>(n));
+  for (int32_t i = 0; i < n; ++i) {
+    if (q_lens[i] < 0) return fail(CS_EINVAL, "negative q_len");
+    if (q_lens[i] > cv[i]->len)
+      return fail(CS_ESTATE, "q_len " + std::to_string(q_lens[i]) + " exceeds conversation length " + std::to_string(cv[i]->len));
+    if (rows + q_lens[i] > INT32_MAX) return fail(CS_EINVAL, "too many query rows");
+    if (q_lens[i] > 0) rc.push_back({static_cast<int32_t>(rows), static_cast<int32_t>(cv[i]->len - q_lens[i])});
+    rows += q_lens[i];
+  }
+  if (rows == 0 || n_layers == 0) return CS_OK;
+  if (!q || !out) return fail(CS_EINVAL, "null q/out");
+  Blob b;
+  b.push(rc.data(), rc.size());
+  if (b.bytes.size() > kQuarter) return fail(CS_ENOMEM, "batch descriptor exceeds the metadata ring");
+  if ((st = ensure_device(p)) != CS_OK) return st;
+  if ((st = use_stream(p, as_stream(stream))) != CS_OK) return st;
+  cs::Meta m;
+  if ((st = place_meta(p, b, &m)) != CS_OK) return st;
+  const cs::PoolGeom g = p->geom();
+  const size_t layer_bytes = static_cast<size_t>(rows) * g.n_q_heads * g.head_dim * 2;
+  const int per = cs::rope_q_layers(g);   // of one launch
+  for (int32_t l = 0; l < n_layers && st == CS_OK; l += per)
+    st = timed_launch(p, CS_PROF_APPEND, "query rotation launch", [&] {
+      return cs::launch_rope_q(g, m, static_cast<int>(rc.size()), rows, std::min(per, n_layers - l), r,
+                               static_cast<const char*>(q) + l * layer_bytes, static_cast<char*>(out) + l * layer_bytes, p->stream);
+    });
+  return st;
+}
+
+cs_status cs_kv_read(cs_pool* p, int32_t n, const cs_conv* convs, const int64_t* starts, const int32_t* counts, void* k, void* v,
+                     cs_stream stream) {
+  if (!p) return fail(CS_EINVAL, "null pool");
+  std::vector<const cs::Conv*> cv;
+  cs_status st = check_convs(p, n, convs, cv);
+  if (st != CS_OK) return st;
+  if (n > 0 && (!starts || !counts)) return fail(CS_EINVAL, "null starts or counts");
+  int64_t total = 0;
+  std::vector<int32_t> slots(n), nn(n);
+  std::vector<int64_t> from(n);
+  std::vector<const std::vector<int32_t>*> lists(n);
+  for (int32_t i = 0; i < n; ++i) {
+    if (counts[i] < 0 || starts[i] < 0) return fail(CS_EINVAL, "negative token range");
+    if (starts[i] > cv[i]->len || counts[i] > cv[i]->len - starts[i])
+      return fail(CS_ERANGE, "token range past the conversation's end");
+    slots[i] = cs::ConvTable::slot_of(convs[i]);
+    from[i] = starts[i];
+    nn[i] = counts[i];
+    lists[i] = &cv[i]->pages;
+    total += counts[i];
+  }
+  if (total == 0) return CS_OK;
+  if (total > INT32_MAX) return fail(CS_EINVAL, "too many tokens in one read");
+  if (!k || !v) return fail(CS_EINVAL, "null k/v");
+  if ((st = ensure_device(p)) != CS_OK) return st;
+  if ((st = use_stream(p, as_stream(stream))) != CS_OK) return st;
+  const std::vector<cs::PageChunk> chunks = cs::plan_append(slots, from, nn, lists);
+  const size_t per = kQuarter / sizeof(cs::PageChunk) - 1;
+  for (size_t c0 = 0; c0 < chunks.size() && st == CS_OK; c0 += per) {
+    const size_t c1 = std::min(chunks.size(), c0 + per);
+    Blob b;
+    b.push(chunks.data() + c0, c1 - c0);
+    cs::Meta m;
+    if ((st = place_meta(p, b, &m)) == CS_OK)
+      st = timed_launch(p, CS_PROF_UNPACK, "read launch", [&] {
+        return cs::launch_read(p->geom(), m, static_cast<int>(c1 - c0), k, v, total, p->stream);
+      });
+  }
+  return st;
 }
 
 cs_status cs_attn_prefill_turn1(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t* q_lens,
@@ -893,24 +1067,41 @@ cs_status cs_kv_pack_size(const cs_pool* p, cs_conv conv, size_t* bytes) {
   if (!p || !bytes) return fail(CS_EINVAL, "null argument");
   const cs::Conv* c = p->convs.find(conv);
   if (!c) return fail(CS_ENOENT, "unknown conversation handle");
-  *bytes = wire_size(p->desc, c->len);
+  *bytes = wire_size(p->desc, p->fp4, c->len);
   return CS_OK;
 }
 
-cs_status cs_kv_pack(const cs_pool* pc, cs_conv conv, void* dst, size_t dst_bytes, cs_stream stream) {
+cs_status cs_kv_pack_fp4_size(const cs_pool* p, cs_conv conv, size_t* bytes) {
+  if (!p || !bytes) return fail(CS_EINVAL, "null argument");
+  const cs::Conv* c = p->convs.find(conv);
+  if (!c) return fail(CS_ENOENT, "unknown conversation handle");
+  *bytes = wire_size(p->desc, true, c->len);
+  return CS_OK;
+}
+
+static cs_status pack_impl(const cs_pool* pc, cs_conv conv, bool fp4, void* dst, size_t dst_bytes, cs_stream stream) {
   cs_pool* p = const_cast<cs_pool*>(pc);  // host metadata is unchanged; stream/ring state is not
   if (!p) return fail(CS_EINVAL, "null pool");
   const cs::Conv* c = p->convs.find(conv);
   if (!c) return fail(CS_ENOENT, "unknown conversation handle");
-  if (dst_bytes != wire_size(p->desc, c->len)) return fail(CS_EINVAL, "dst_bytes != cs_kv_pack_size");
+  if (dst_bytes != wire_size(p->desc, fp4, c->len)) return fail(CS_EINVAL, "dst_bytes is not the conversation's wire size");
   if (c->len == 0) return CS_OK;
   if (!dst) return fail(CS_EINVAL, "null dst");
   cs_status st;
   if ((st = ensure_device(p)) != CS_OK) return st;
   if ((st = use_stream(p, as_stream(stream))) != CS_OK) return st;
   return timed_launch(p, CS_PROF_PACK, "pack launch", [&] {
-    return cs::launch_pack(p->geom(), cs::ConvTable::slot_of(conv), c->len, dst, p->stream);
+    return fp4 ? cs::launch_pack_fp4(p->geom(), cs::ConvTable::slot_of(conv), c->len, dst, p->stream)
+               : cs::launch_pack(p->geom(), cs::ConvTable::slot_of(conv), c->len, dst, p->stream);
   });
+}
+
+cs_status cs_kv_pack(const cs_pool* p, cs_conv conv, void* dst, size_t dst_bytes, cs_stream stream) {
+  return pack_impl(p, conv, p && p->fp4, dst, dst_bytes, stream);
+}
+
+cs_status cs_kv_pack_fp4(const cs_pool* p, cs_conv conv, void* dst, size_t dst_bytes, cs_stream stream) {
+  return pack_impl(p, conv, true, dst, dst_bytes, stream);
 }
 
 cs_status cs_kv_unpack(cs_pool* p, const void* src, size_t src_bytes, int64_t n_tokens,
@@ -920,7 +1111,7 @@ cs_status cs_kv_unpack(cs_pool* p, const void* src, size_t src_bytes, int64_t n_
   if (!src) return fail(CS_EINVAL, "null src");
   const int64_t np = cs::pages_for(n_tokens);
   if (np > p->desc.max_pages_per_conv) return fail(CS_ERANGE, "conversation exceeds max_pages_per_conv");
-  if (src_bytes != wire_size(p->desc, n_tokens))
+  if (src_bytes != wire_size(p->desc, p->fp4, n_tokens))
     return fail(CS_EINVAL, "src_bytes does not match the wire size of n_tokens for this pool");
   if (p->convs.live_count() >= p->convs.max_convs()) return fail(CS_ENOMEM, "all conversation slots are live");
   if (np > p->pages.free_count()) return fail(CS_ENOMEM, "KV pool exhausted");
@@ -941,6 +1132,9 @@ cs_status cs_kv_unpack(cs_pool* p, const void* src, size_t src_bytes, int64_t n_
     cs::Meta m;
     if ((st = place_meta(p, b, &m)) != CS_OK) return st;
     st = timed_launch(p, CS_PROF_UNPACK, "unpack launch", [&] {
+      if (p->fp4)
+        return cs::launch_unpack_fp4(p->geom(), src, m, cs::ConvTable::slot_of(h), n_tokens, static_cast<int>(p0),
+                                     static_cast<int>(p1 - p0), p->stream);
       return cs::launch_unpack(p->geom(), src, m, cs::ConvTable::slot_of(h),
                                n_tokens, static_cast<int>(p0), static_cast<int>(p1 - p0), p->stream);
     });
@@ -1003,7 +1197,8 @@ cs_status cs_mixed_step(cs_pool* p, int32_t n_ext, const cs_conv* ext_convs, con
   }
   cs::ExtendPlan e_plan = plan_extend_batch(p, e_slots, e_lens, e_q);
   const bool ordered = (flags & CS_MIXED_LAYER_ORDERED) != 0;
-  const float dec_steps = cs::decode_steps(d_lens, p->desc.n_kv_heads, p->desc.head_dim, cs::kCus);
+  const float dec_steps = cs::decode_steps(d_lens, p->desc.n_kv_heads, p->desc.head_dim, cs::kCus) *
+                          static_cast<float>(block_bytes(p->desc, p->fp4)) / static_cast<float>(block_bytes(p->desc, false));
   if (cs::chain_pays(e_plan, p->desc.n_kv_heads, cs::kCus, ordered ? 1 : p->desc.n_layers, dec_steps))
     cs::chain_extend(e_plan);
   Blob blob;

@@ -62,6 +62,13 @@ __global__ __launch_bounds__(kDecodeItemThreads) void decode_split_kernel(Launch
   split_body<D>(a, blockIdx.x, blockIdx.y, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), xch);
 }
 
+// the same over 4-bit pages
+template <int D>
+__global__ __launch_bounds__(kDecodeItemThreads) void decode_split_fp4_kernel(LaunchMeta, DecodeArgs a) {
+  __shared__ float xch[split_exchange_floats<D>()];
+  split_body<D, true>(a, blockIdx.x, blockIdx.y, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), xch);
+}
+
 template <int D>
 __global__ __launch_bounds__(256) void decode_merge_kernel(LaunchMeta, DecodeArgs a) {
   __shared__ MergeLds<D> lds;
@@ -78,7 +85,9 @@ hipError_t launch_decode_split(const PoolGeom& g, int layer, int n_layers, const
   LaunchMeta m;
   fill_meta(w.meta, &m);
   const dim3 grid(w.n_items * g.n_kv_heads, n_layers);
-  if (g.head_dim == 128) decode_split_kernel<128><<<grid, kDecodeItemThreads, 0, stream>>>(m, a);
+  if (g.head_dim == 128 && g.fp4) decode_split_fp4_kernel<128><<<grid, kDecodeItemThreads, 0, stream>>>(m, a);
+  else if (g.head_dim == 64 && g.fp4) decode_split_fp4_kernel<64><<<grid, kDecodeItemThreads, 0, stream>>>(m, a);
+  else if (g.head_dim == 128) decode_split_kernel<128><<<grid, kDecodeItemThreads, 0, stream>>>(m, a);
   else if (g.head_dim == 64) decode_split_kernel<64><<<grid, kDecodeItemThreads, 0, stream>>>(m, a);
   else return hipErrorInvalidValue;
   return hipGetLastError();

@@ -5,6 +5,7 @@
 #include <cmath>
 
 #include "device_common.hpp"
+#include "fp4.hpp"
 #include "kernels.hpp"
 
 namespace cs {
@@ -68,7 +69,8 @@ constexpr int split_exchange_floats() { return (kDecodeSubSplits - 1) * 8 * (D +
 // in the order w = 0, 1, ... and writes the item's one partial record: far fewer, larger writes
 // interleaved with the KV stream than one record per wave (the HBM reads run 7% faster with 8
 // waves per item than with one). Every wave reaches the one barrier, also one that has no keys.
-template <int D>
+// FP4: the pool's blocks hold 4-bit codes (fp4.hpp).
+template <int D, bool FP4 = false>
 __device__ __forceinline__ void split_body(const DecodeArgs& a, const int work, const int dl, const int wave,
                                            float* xch) {
   constexpr int KS = D / 32;  // k-steps of the QK^T contraction
@@ -90,14 +92,15 @@ __device__ __forceinline__ void split_body(const DecodeArgs& a, const int work, 
   const int c = lane & 15;   // MFMA column: query head within the group; A-operand row: key / dim
   const int qd = lane >> 4;  // k-block of the lane (8 consecutive k values)
 
-  // Query operand: head c of this kv head's group, dims 32*ks + 8*qd .. +8.
+  // Query operand: head c of this kv head's group, dims 32*ks + 8*qd .. +8 (4-bit pages: (D/4) qd + 8 ks,
+  // so that a lane's K dims are consecutive).
   const int n_q_heads = a.n_kv_heads * a.group;
   bf16x8 qop[KS];
   {
     const uint16_t* qrow = a.q + (static_cast<size_t>(dl * a.n_convs + conv_idx) * n_q_heads + g * a.group + c) * D;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
-      qop[ks] = c < a.group ? as_bf16x8(ld16(qrow + 32 * ks + 8 * qd)) : bf16x8{};
+      qop[ks] = c < a.group ? as_bf16x8(ld16(FP4 ? qrow + 8 * ks + D / 4 * qd : qrow + 32 * ks + 8 * qd)) : bf16x8{};
   }
 
   const int pid = lane < n_pg ? pt[lane] : 0;
@@ -106,87 +109,176 @@ __device__ __forceinline__ void split_body(const DecodeArgs& a, const int work, 
 #pragma unroll
   for (int t = 0; t < DT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  const size_t head_stride = static_cast<size_t>(2 * kPageTokens * D);
-  const uint16_t* layer_base = a.pool + static_cast<size_t>(a.layer + dl) * a.n_pages * a.n_kv_heads * head_stride +
-                               static_cast<size_t>(g) * head_stride;
-  const size_t page_stride = static_cast<size_t>(a.n_kv_heads) * head_stride;
-  // Per-lane byte offsets inside a page block (the same for every page): key c, dims 8 qd ..
-  // (+32 ks: next K sub-block, 1 KiB on); V^T row c (of a 16-dim tile), keys 4 qd .. 4 qd + 3.
-  const uint32_t koff = static_cast<uint32_t>((c * 32 + 8 * qd) * 2);
-  const uint32_t voff = static_cast<uint32_t>((kPageTokens * D + c * kPageTokens + 4 * qd) * 2);
-
-  for (int j = 0; j < n_pg; j += 2) {
-    const bool has_b = j + 1 < n_pg;
-    const int pa = __builtin_amdgcn_readlane(pid, j);
-    const int pb = has_b ? __builtin_amdgcn_readlane(pid, j + 1) : pa;
-    const uint8_t* blk_a = reinterpret_cast<const uint8_t*>(layer_base + static_cast<size_t>(pa) * page_stride);
-    const uint8_t* blk_b = reinterpret_cast<const uint8_t*>(layer_base + static_cast<size_t>(pb) * page_stride);
-
-    bf16x8 ka[KS], kb[KS];
-    uint2 va[DT], vb[DT];
+  if constexpr (FP4) {
+    using B = Fp4Block<D>;
+    constexpr int NW = B::kWords;
+    const size_t page_stride = static_cast<size_t>(a.n_kv_heads) * B::kBytes;
+    const uint8_t* base = reinterpret_cast<const uint8_t*>(a.pool) + static_cast<size_t>(a.layer + dl) * a.n_pages * page_stride +
+                          static_cast<size_t>(g) * B::kBytes;
+    struct Page {
+      uint32_t k[NW], v[NW], ks, vs;
+    };
+    auto load = [&](int j) {
+      Page p;
+      const uint8_t* blk = base + static_cast<size_t>(__builtin_amdgcn_readlane(pid, j)) * page_stride;
+      if constexpr (D == 128) {
+        const uint4 k = ld16_nt(blk + B::kK + 16 * lane), v = ld16_nt(blk + B::kV + 16 * lane);
+        p.k[0] = k.x, p.k[1] = k.y, p.k[2] = k.z, p.k[3] = k.w;
+        p.v[0] = v.x, p.v[1] = v.y, p.v[2] = v.z, p.v[3] = v.w;
+      } else {
+        const uint2 k = ld8_nt(blk + B::kK + 8 * lane), v = ld8_nt(blk + B::kV + 8 * lane);
+        p.k[0] = k.x, p.k[1] = k.y;
+        p.v[0] = v.x, p.v[1] = v.y;
+      }
+      p.ks = blk[B::k_scale(qd, c)];
+      p.vs = *reinterpret_cast<const uint32_t*>(blk + B::kVScale + 4 * qd);
+      return p;
+    };
+    Page na = load(0), nb = load(n_pg > 1 ? 1 : 0);
+    for (int j = 0; j < n_pg; j += 2) {
+      const Page pa = na, pb = nb;
+      // the next page pair (the last one again at the end): its loads fly during this pair's arithmetic
+      na = load(min(j + 2, n_pg - 1));
+      nb = load(min(j + 3, n_pg - 1));
+      f32x4 sa = {0.f, 0.f, 0.f, 0.f}, sb = {0.f, 0.f, 0.f, 0.f};
+      const float ksa = fp4_scale(pa.ks), ksb = fp4_scale(pb.ks);
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) ka[ks] = as_bf16x8(ld16_nt(blk_a + koff + 1024 * ks));
+      for (int ks = 0; ks < KS; ++ks) {
+        sa = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(fp4_word(pa.k[ks], ksa)), qop[ks], sa, 0, 0, 0);
+        sb = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(fp4_word(pb.k[ks], ksb)), qop[ks], sb, 0, 0, 0);
+      }
+      // sa[r]: head c, key k_begin + 16j + 4qd + r; sb[r]: the same + 16.
+      const int key_a = k_begin + kPageTokens * j + 4 * qd;
+      float x[8], vs[8];
 #pragma unroll
-    for (int t = 0; t < DT; ++t) va[t] = ld8_nt(blk_a + voff + 16 * kPageTokens * 2 * t);
-    if (has_b) {
+      for (int r = 0; r < 4; ++r) {
+        x[r] = sa[r] * a.scale_log2;
+        x[4 + r] = sb[r] * a.scale_log2;
+        vs[r] = fp4_scale_of(pa.vs, r);
+        vs[4 + r] = fp4_scale_of(pb.vs, r);
+      }
+      if (k_begin + kPageTokens * (j + 2) > k_end) {
+        // keys past the wave's range: weight 0, and 0 for the scale too (0 x a scale of 255 would be NaN)
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) kb[ks] = as_bf16x8(ld16_nt(blk_b + koff + 1024 * ks));
+        for (int r = 0; r < 8; ++r) {
+          const bool in = key_a + (r < 4 ? r : kPageTokens + r - 4) < k_end;
+          x[r] = in ? x[r] : -INFINITY;
+          vs[r] = in ? vs[r] : 0.f;
+        }
+      }
+      float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+      mx = fmaxf(mx, xor_shfl(mx, 16));
+      mx = fmaxf(mx, xor_shfl(mx, 32));
+      const float m_new = fmaxf(m_run, mx);
+      if (__builtin_amdgcn_ballot_w64(m_new > m_run) != 0) {
+        const float alpha = fast_exp2(m_run - m_new);
+        l_run *= alpha;
 #pragma unroll
-      for (int t = 0; t < DT; ++t) vb[t] = ld8_nt(blk_b + voff + 16 * kPageTokens * 2 * t);
-    } else {
+        for (int t = 0; t < DT; ++t) o[t] *= alpha;
+        m_run = m_new;
+      }
+      float p[8];
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) kb[ks] = bf16x8{};
+      for (int r = 0; r < 8; ++r) p[r] = fast_exp2(x[r] - m_run);
+      const uint4 pw = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
+      // The denominator sums the same bf16-rounded weights the PV product uses: scaling by the values' power
+      // of two commutes with the rounding.
+      l_run += (sum_bf16x2(pw.x) + sum_bf16x2(pw.y)) + (sum_bf16x2(pw.z) + sum_bf16x2(pw.w));
+      const bf16x8 pop = as_bf16x8(make_uint4(pack_bf16x2(p[0] * vs[0], p[1] * vs[1]), pack_bf16x2(p[2] * vs[2], p[3] * vs[3]),
+                                              pack_bf16x2(p[4] * vs[4], p[5] * vs[5]), pack_bf16x2(p[6] * vs[6], p[7] * vs[7])));
 #pragma unroll
-      for (int t = 0; t < DT; ++t) vb[t] = make_uint2(0, 0);
-    }
-
-    f32x4 sa = {0.f, 0.f, 0.f, 0.f}, sb = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      sa = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[ks], qop[ks], sa, 0, 0, 0);
-      sb = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb[ks], qop[ks], sb, 0, 0, 0);
-    }
-    // sa[r]: head c, key k_begin + 16j + 4qd + r; sb[r]: the same + 16.
-    const int key_a = k_begin + kPageTokens * j + 4 * qd;
-    float xa[4], xb[4];
-    float mx = -INFINITY;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      xa[r] = key_a + r < k_end ? sa[r] * a.scale_log2 : -INFINITY;
-      xb[r] = key_a + kPageTokens + r < k_end ? sb[r] * a.scale_log2 : -INFINITY;
-      mx = fmaxf(mx, fmaxf(xa[r], xb[r]));
-    }
-    mx = fmaxf(mx, xor_shfl(mx, 16));
-    mx = fmaxf(mx, xor_shfl(mx, 32));
-    const float m_new = fmaxf(m_run, mx);
-    const float alpha = fast_exp2(m_run - m_new);
-    float pa_[4], pb_[4];
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      pa_[r] = fast_exp2(xa[r] - m_new);
-      pb_[r] = fast_exp2(xb[r] - m_new);
-    }
-    const uint4 pw = make_uint4(pack_bf16x2(pa_[0], pa_[1]), pack_bf16x2(pa_[2], pa_[3]),
-                                pack_bf16x2(pb_[0], pb_[1]), pack_bf16x2(pb_[2], pb_[3]));
-    // The denominator sums the same bf16-rounded weights the PV product uses.
-    const float psum = (sum_bf16x2(pw.x) + sum_bf16x2(pw.y)) + (sum_bf16x2(pw.z) + sum_bf16x2(pw.w));
-    l_run = l_run * alpha + psum;
-    m_run = m_new;
-    const bf16x8 pop = __builtin_bit_cast(bf16x8, pw);
-    if (k_begin + kPageTokens * (j + 2) > cd.len) {
-      // Last page pair of the conversation: zero V of keys >= len so nothing past the end leaks.
-#pragma unroll
-      for (int t = 0; t < DT; ++t) {
-        va[t].x = mask_bf16x2(va[t].x, key_a + 0 < cd.len, key_a + 1 < cd.len);
-        va[t].y = mask_bf16x2(va[t].y, key_a + 2 < cd.len, key_a + 3 < cd.len);
-        vb[t].x = mask_bf16x2(vb[t].x, key_a + 16 < cd.len, key_a + 17 < cd.len);
-        vb[t].y = mask_bf16x2(vb[t].y, key_a + 18 < cd.len, key_a + 19 < cd.len);
+      for (int w = 0; w < NW; ++w) {
+        o[2 * w] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+            as_bf16x8(make_uint2(fp4_pair<0>(pa.v[w], 1.f), fp4_pair<1>(pa.v[w], 1.f)),
+                      make_uint2(fp4_pair<0>(pb.v[w], 1.f), fp4_pair<1>(pb.v[w], 1.f))), pop, o[2 * w], 0, 0, 0);
+        o[2 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+            as_bf16x8(make_uint2(fp4_pair<2>(pa.v[w], 1.f), fp4_pair<3>(pa.v[w], 1.f)),
+                      make_uint2(fp4_pair<2>(pb.v[w], 1.f), fp4_pair<3>(pb.v[w], 1.f))), pop, o[2 * w + 1], 0, 0, 0);
       }
     }
+  } else {
+    const size_t head_stride = static_cast<size_t>(2 * kPageTokens * D);
+    const uint16_t* layer_base = a.pool + static_cast<size_t>(a.layer + dl) * a.n_pages * a.n_kv_heads * head_stride +
+                                 static_cast<size_t>(g) * head_stride;
+    const size_t page_stride = static_cast<size_t>(a.n_kv_heads) * head_stride;
+    // Per-lane byte offsets inside a page block (the same for every page): key c, dims 8 qd ..
+    // (+32 ks: next K sub-block, 1 KiB on); V^T row c (of a 16-dim tile), keys 4 qd .. 4 qd + 3.
+    const uint32_t koff = static_cast<uint32_t>((c * 32 + 8 * qd) * 2);
+    const uint32_t voff = static_cast<uint32_t>((kPageTokens * D + c * kPageTokens + 4 * qd) * 2);
+
+    for (int j = 0; j < n_pg; j += 2) {
+      const bool has_b = j + 1 < n_pg;
+      const int pa = __builtin_amdgcn_readlane(pid, j);
+      const int pb = has_b ? __builtin_amdgcn_readlane(pid, j + 1) : pa;
+      const uint8_t* blk_a = reinterpret_cast<const uint8_t*>(layer_base + static_cast<size_t>(pa) * page_stride);
+      const uint8_t* blk_b = reinterpret_cast<const uint8_t*>(layer_base + static_cast<size_t>(pb) * page_stride);
+
+      bf16x8 ka[KS], kb[KS];
+      uint2 va[DT], vb[DT];
 #pragma unroll
-    for (int t = 0; t < DT; ++t) {
-      o[t] *= alpha;
-      o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(va[t], vb[t]), pop, o[t], 0, 0, 0);
+      for (int ks = 0; ks < KS; ++ks) ka[ks] = as_bf16x8(ld16_nt(blk_a + koff + 1024 * ks));
+#pragma unroll
+      for (int t = 0; t < DT; ++t) va[t] = ld8_nt(blk_a + voff + 16 * kPageTokens * 2 * t);
+      if (has_b) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) kb[ks] = as_bf16x8(ld16_nt(blk_b + koff + 1024 * ks));
+#pragma unroll
+        for (int t = 0; t < DT; ++t) vb[t] = ld8_nt(blk_b + voff + 16 * kPageTokens * 2 * t);
+      } else {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) kb[ks] = bf16x8{};
+#pragma unroll
+        for (int t = 0; t < DT; ++t) vb[t] = make_uint2(0, 0);
+      }
+
+      f32x4 sa = {0.f, 0.f, 0.f, 0.f}, sb = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        sa = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[ks], qop[ks], sa, 0, 0, 0);
+        sb = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb[ks], qop[ks], sb, 0, 0, 0);
+      }
+      // sa[r]: head c, key k_begin + 16j + 4qd + r; sb[r]: the same + 16.
+      const int key_a = k_begin + kPageTokens * j + 4 * qd;
+      float xa[4], xb[4];
+      float mx = -INFINITY;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        xa[r] = key_a + r < k_end ? sa[r] * a.scale_log2 : -INFINITY;
+        xb[r] = key_a + kPageTokens + r < k_end ? sb[r] * a.scale_log2 : -INFINITY;
+        mx = fmaxf(mx, fmaxf(xa[r], xb[r]));
+      }
+      mx = fmaxf(mx, xor_shfl(mx, 16));
+      mx = fmaxf(mx, xor_shfl(mx, 32));
+      const float m_new = fmaxf(m_run, mx);
+      const float alpha = fast_exp2(m_run - m_new);
+      float pa_[4], pb_[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        pa_[r] = fast_exp2(xa[r] - m_new);
+        pb_[r] = fast_exp2(xb[r] - m_new);
+      }
+      const uint4 pw = make_uint4(pack_bf16x2(pa_[0], pa_[1]), pack_bf16x2(pa_[2], pa_[3]),
+                                  pack_bf16x2(pb_[0], pb_[1]), pack_bf16x2(pb_[2], pb_[3]));
+      // The denominator sums the same bf16-rounded weights the PV product uses.
+      const float psum = (sum_bf16x2(pw.x) + sum_bf16x2(pw.y)) + (sum_bf16x2(pw.z) + sum_bf16x2(pw.w));
+      l_run = l_run * alpha + psum;
+      m_run = m_new;
+      const bf16x8 pop = __builtin_bit_cast(bf16x8, pw);
+      if (k_begin + kPageTokens * (j + 2) > cd.len) {
+        // Last page pair of the conversation: zero V of keys >= len so nothing past the end leaks.
+#pragma unroll
+        for (int t = 0; t < DT; ++t) {
+          va[t].x = mask_bf16x2(va[t].x, key_a + 0 < cd.len, key_a + 1 < cd.len);
+          va[t].y = mask_bf16x2(va[t].y, key_a + 2 < cd.len, key_a + 3 < cd.len);
+          vb[t].x = mask_bf16x2(vb[t].x, key_a + 16 < cd.len, key_a + 17 < cd.len);
+          vb[t].y = mask_bf16x2(vb[t].y, key_a + 18 < cd.len, key_a + 19 < cd.len);
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < DT; ++t) {
+        o[t] *= alpha;
+        o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(va[t], vb[t]), pop, o[t], 0, 0, 0);
+      }
     }
   }
   // l_run holds this lane's keys only; sum over the four k-blocks of the column.

@@ -18,6 +18,7 @@ struct PoolGeom {
   int head_dim;
   int32_t* page_table;  // device mirror [max_convs][max_pages]
   int max_pages;
+  bool fp4;             // blocks of 4-bit codes and scales (fp4.hpp) instead of bf16
 };
 
 // Metadata of one launch (descriptors, work lists, page ids): `bytes` bytes laid out on the host at
@@ -55,6 +56,39 @@ struct AppendCarry {
 };
 hipError_t launch_append(const PoolGeom& g, const Meta& meta, int n_chunks, const AppendCarry& carry,
                          const void* k, const void* v, int64_t src_rows, hipStream_t stream);
+
+// Rotation of the first 2 pairs dims of a head (rope.hpp): per pair the 64-bit fraction of a turn a
+// position makes.
+struct RopeArgs {
+  uint64_t frac[64];
+  float amplitude;
+  int pairs;        // a multiple of 8, at most head_dim / 2
+  int interleaved;  // pair i = dims 2 i, 2 i + 1; else dims i, i + pairs
+};
+
+// The append of 4-bit pools, and of both kinds with rotated keys (rope != nullptr). With q != nullptr the
+// launch also writes the rotated q [n_layers][src_rows][Hq][D] to q_out (may be q itself).
+hipError_t launch_append_as(const PoolGeom& g, const Meta& meta, int n_chunks, const AppendCarry& carry, const RopeArgs* rope,
+                            const void* k, const void* v, const void* q, void* q_out, int64_t src_rows, hipStream_t stream);
+
+// Rotation of query rows q [n_layers][rows][Hq][D] into out (may be q): meta = RopeConv[n_convs].
+struct RopeConv {
+  int32_t row;   // first row of the conversation
+  int32_t pos;   // its position
+};
+hipError_t launch_rope_q(const PoolGeom& g, const Meta& meta, int n_convs, int64_t rows, int n_layers, const RopeArgs& rope,
+                         const void* q, void* out, hipStream_t stream);
+
+// Layers one such launch may take (a grid dimension).
+int rope_q_layers(const PoolGeom& g);
+
+// Read back: chunks (meta: PageChunk[n_chunks]) of the pool to k, v [n_layers][dst_rows][Hkv][D] in bf16.
+hipError_t launch_read(const PoolGeom& g, const Meta& meta, int n_chunks, void* k, void* v, int64_t dst_rows, hipStream_t stream);
+
+// Pack of a conversation (of a pool of either kind) into the wire of a 4-bit pool, and that pool's unpack.
+hipError_t launch_pack_fp4(const PoolGeom& g, int slot, int64_t len, void* wire, hipStream_t stream);
+hipError_t launch_unpack_fp4(const PoolGeom& g, const void* wire, const Meta& meta, int slot, int64_t len, int lp0, int n_lp,
+                             hipStream_t stream);
 
 // Pack: conversation pages (page-table row `slot`) -> wire [layer][lpage][head] blocks.
 hipError_t launch_pack(const PoolGeom& g, int slot, int64_t len, void* wire, hipStream_t stream);
