@@ -6,9 +6,9 @@ largest magnitude, at least 2^-126, so that the largest e2m1 value, 6, is reache
 nearest, ties to the even code, and saturate at 6.
 
 Wire: [layer][logical page][kv head] blocks of 17 d bytes: two 4-bit codes a byte, the first in the low
-bits, K as [4][16 tokens][d/4 dims], V as [4][16 rows c][d/16 tiles t][4 tokens] (part i: dim 16 t + c of
-tokens 4 i ..); then the powers as bytes e (2^(e - 127)): K [d/32][16 tokens], V [16 tokens]; zeros up to
-17 d. Token slots past the end are zeros.
+bits, K as [d/32 groups][16 tokens][32 dims], V as [4][16 rows c][d/16 tiles t][4 tokens] (part i: dim
+16 t + c of tokens 4 i ..); then the powers as bytes e (2^(e - 127)): K [16 tokens][d/32], V [16 tokens];
+zeros up to 17 d. Token slots past the end are zeros.
 """
 from __future__ import annotations
 
@@ -66,11 +66,11 @@ def serialize(k: np.ndarray, v: np.ndarray) -> np.ndarray:
         a = a.reshape(nl, n_pages, hkv, -1)
         return (a[..., 0::2] + 16 * a[..., 1::2]).astype(np.uint8)
 
-    kp = paged(kc).reshape(nl, n_pages, hkv, PAGE, 4, d // 4)
+    kp = paged(kc).reshape(nl, n_pages, hkv, PAGE, d // 32, 32)
     out[..., :8 * d] = nibbles(np.moveaxis(kp, 4, 3))
     vp = paged(vc).reshape(nl, n_pages, hkv, 4, 4, d // 16, 16)          # [i][token of i][t][c]
     out[..., 8 * d:16 * d] = nibbles(vp.transpose(0, 1, 2, 3, 6, 5, 4))   # [i][c][t][token]
     n_k = PAGE * d // 32
-    out[..., 16 * d:16 * d + n_k] = np.swapaxes(paged(ke + 127), 3, 4).reshape(nl, n_pages, hkv, -1)
+    out[..., 16 * d:16 * d + n_k] = paged(ke + 127).reshape(nl, n_pages, hkv, -1)
     out[..., 16 * d + n_k:16 * d + n_k + PAGE] = paged(ve + 127).reshape(nl, n_pages, hkv, PAGE)
     return out.reshape(-1)

@@ -131,8 +131,9 @@ __device__ __forceinline__ void lds_wait_barrier() { asm volatile("s_waitcnt lgk
 // the loop costs launches without such tiles 1.5%).
 //
 // FP4: the pool's blocks hold 4-bit codes (fp4.hpp). They pass through registers instead of the copies above: a
-// wave loads half of a page's K and V codes and their scales a step ahead, converts them at the start of the
-// next and writes them to the ring as the bf16 tile that the other form copies; everything else is the same.
+// wave loads half of a page's K and V codes and their scales a step ahead and writes them to the ring at the
+// start of the next step, K as it is (its codes and scales are operands of the MX matrix instructions), V
+// converted to the bf16 tile that the other form copies. Everything behind the scores is the same.
 template <int D, int G, bool PRE, bool CHAIN, bool FP4 = false>
 __device__ __forceinline__ void attn_fwd_block(const ExtendArgs& a, const int block, const int dl) {
   constexpr int NW = 8;                   // waves: G query heads x (8 / G) blocks of 32 queries
@@ -150,8 +151,11 @@ __device__ __forceinline__ void attn_fwd_block(const ExtendArgs& a, const int bl
   // chunk swizzle of LDS row r
   auto swz = [](int r) { return D == 128 ? r & 15 : (r >> 1) & 7; };
   constexpr int NBUF = 4;                 // LDS ring: tile j read, j+1 landed, j+2 and j+3 in flight
-  constexpr int VBASE = NBUF * HALF_TILE; // V^T parts after the K parts of all buffers
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * NBUF * HALF_TILE];
+  constexpr int KBUF = FP4 ? 4 * 8 * D : HALF_TILE;   // K bytes per buffer
+  constexpr int SBASE = NBUF * KBUF, SBUF = FP4 ? 4 * D / 2 : 0;   // K scales of 4-bit pages after them
+  constexpr int VBASE = SBASE + NBUF * SBUF;          // V^T parts after the K parts of all buffers
+  constexpr int LDS = VBASE + NBUF * HALF_TILE;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[LDS];
 
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int tile_idx = block / a.n_kv_heads, g = block % a.n_kv_heads;
@@ -200,20 +204,22 @@ __device__ __forceinline__ void attn_fwd_block(const ExtendArgs& a, const int bl
   // conversation's end are its last page), so every step issues the same number and the counter
   // waits below stay exact. Those keys are masked by the causal mask.
   auto page_of = [&](int j) { return ptc[min(4 * min(j, n_kt - 1) + q_w, n_pg - 1)]; };
-  // 4-bit pages: this wave's half of a page (its dims' half of each lane's words) and where it goes.
+  // 4-bit pages: this wave's half of a page (half of its K, of its K scales, and of each lane's V words) and
+  // where it goes.
   using B4 = Fp4Block<D>;
   constexpr int NH = B4::kWords / 2;      // words of K, and of V, a lane takes
   struct Codes {
     uint32_t k[NH], v[NH], ks, vs;
   };
   const int f_c = lane & 15, f_qd = lane >> 4, f_h = wave & 1;
+  const bool f_scales = lane < D / 16;    // lanes that take a word of the K scales
   const uint8_t* f_base = reinterpret_cast<const uint8_t*>(a.pool) +
                           (static_cast<size_t>(a.layer + dl) * a.n_pages * a.n_kv_heads + g) * B4::kBytes;
   const size_t f_stride = static_cast<size_t>(a.n_kv_heads) * B4::kBytes;
   auto load_codes = [&](int page) {
     Codes x;
     const uint8_t* blk = f_base + static_cast<size_t>(page) * f_stride;
-    const uint8_t* kc = blk + B4::kK + (lane * B4::kWords + f_h * NH) * 4;
+    const uint8_t* kc = blk + B4::kK + f_h * 4 * D + lane * 4 * NH;
     const uint8_t* vc = blk + B4::kV + (lane * B4::kWords + f_h * NH) * 4;
     if constexpr (NH == 2) {
       const uint2 kk = ld8(kc), vv = ld8(vc);
@@ -222,23 +228,18 @@ __device__ __forceinline__ void attn_fwd_block(const ExtendArgs& a, const int bl
       x.k[0] = *reinterpret_cast<const uint32_t*>(kc);
       x.v[0] = *reinterpret_cast<const uint32_t*>(vc);
     }
-    x.ks = blk[B4::k_scale(f_qd, f_c)];
+    if (f_scales) x.ks = *reinterpret_cast<const uint32_t*>(blk + B4::kKScale + f_h * (D / 4) + lane * 4);
     x.vs = *reinterpret_cast<const uint32_t*>(blk + B4::kVScale + 4 * f_qd);
     return x;
   };
-  // K row of key f_c (bits 2 and 3 swapped, as above), chunks (D / 32) f_qd + NH f_h + i; V^T dims
-  // 16 (2 NH f_h + t) + f_c, keys 4 f_qd .. + 3.
-  const int f_row = (f_c & 3) | ((f_c >> 3) & 1) << 2 | ((f_c >> 2) & 1) << 3;
-  const uint32_t f_krow = static_cast<uint32_t>((kPageTokens * q_w + f_row) * (2 * D));
+  // V^T dims 16 (2 NH f_h + t) + f_c, keys 4 f_qd .. + 3
   const uint32_t f_v = static_cast<uint32_t>(q_w * (kPageTokens * 2 * D) + (32 * NH * f_h + f_c) * 32 +
                                              (((f_qd >> 1) ^ ((f_c >> 2) & 1) ^ ((f_c >> 3) & 1)) * 16) + (f_qd & 1) * 8);
   auto store_codes = [&](const Codes& x, int buf) {
-    const float ks = fp4_scale(x.ks);
-#pragma unroll
-    for (int i = 0; i < NH; ++i) {
-      const int chunk = (B4::kWords * f_qd + NH * f_h + i) ^ swz(f_row);
-      st16(smem + buf * HALF_TILE + f_krow + chunk * 16, fp4_word(x.k[i], ks));
-    }
+    uint8_t* kd = smem + buf * KBUF + q_w * 8 * D + f_h * 4 * D + lane * 4 * NH;
+    if constexpr (NH == 2) st8(kd, make_uint2(x.k[0], x.k[1]));
+    else *reinterpret_cast<uint32_t*>(kd) = x.k[0];
+    if (f_scales) *reinterpret_cast<uint32_t*>(smem + SBASE + buf * SBUF + q_w * (D / 2) + f_h * (D / 4) + lane * 4) = x.ks;
     const float vs[4] = {fp4_scale_of(x.vs, 0), fp4_scale_of(x.vs, 1), fp4_scale_of(x.vs, 2), fp4_scale_of(x.vs, 3)};
 #pragma unroll
     for (int i = 0; i < NH; ++i) {   // (16 dims on: 512 bytes; bits 2 and 3 of the dim are f_c's)
@@ -277,8 +278,17 @@ __device__ __forceinline__ void attn_fwd_block(const ExtendArgs& a, const int bl
   const int qpos = prefix + (valid ? qrow0 + col : cd.q_len - 1);
   const uint16_t* qrow =
       a.q + dl * a.q_stride + (static_cast<size_t>(cd.q_row + (valid ? qrow0 + col : 0)) * n_q_heads + h) * D;
+  constexpr int KM = D / 64;              // k-steps of the MX score product
+  uint4 q4[KM][4];
+  if constexpr (FP4) {
 #pragma unroll
-  for (int ks = 0; ks < KS; ++ks) qop[ks] = as_bf16x8(ld16(qrow + 16 * ks + 8 * half));  // padding rows: row 0
+    for (int ks = 0; ks < KM; ++ks)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) q4[ks][i] = ld16(qrow + 64 * ks + 32 * half + 8 * i);
+  } else {
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qop[ks] = as_bf16x8(ld16(qrow + 16 * ks + 8 * half));  // padding rows: row 0
+  }
   // (one vector load of the first four tiles' pages: one trip to memory instead of four)
   const int pages = pt[min(4 * min(kt0 + (lane & 3), n_kt - 1) + q_w, n_pg - 1)];
   Codes first[2];
@@ -295,10 +305,16 @@ __device__ __forceinline__ void attn_fwd_block(const ExtendArgs& a, const int bl
   // Q must have arrived before the loop: a wait of the compiler's at the loop head would drain the copies
   // that the loop keeps in flight. Here too its waits do not count the copies (made in asm) and so wait
   // for all three tiles behind Q, though the barrier below needs only two.
+  Bf6Query query[KM];
+  if constexpr (FP4) {
 #pragma unroll
-  for (int ks = 0; ks < KS; ++ks) {
-    if (!valid) qop[ks] = bf16x8{};
-    asm volatile("" ::"v"(qop[ks]));
+    for (int ks = 0; ks < KM; ++ks) query[ks] = split_query(q4[ks]);   // padding rows: row 0's (not stored)
+  } else {
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      if (!valid) qop[ks] = bf16x8{};
+      asm volatile("" ::"v"(qop[ks]));
+    }
   }
   f32x16 o[DT];
 #pragma unroll
@@ -345,13 +361,34 @@ __device__ __forceinline__ void attn_fwd_block(const ExtendArgs& a, const int bl
   auto v_operand = [&](int buf, int kt2, int j2, int t) {
     return as_bf16x8(ld16(smem + VBASE + buf * HALF_TILE + vaddr + (DT * (2 * kt2 + j2) + t) * 1024));
   };
+  // 4-bit pages: K rows col of pages 2 kt2 and 2 kt2 + 1 (their key order as above), dims 64 ks + 32 half ..;
+  // the row's scales, this half's group in byte 2 ks
+  const int f_row = (col & 3) | ((col >> 3) & 1) << 2 | ((col >> 2) & 1) << 3;
+  const uint32_t mx_addr = static_cast<uint32_t>((col >> 4) * 8 * D + half * 256 + f_row * 16);
+  const uint32_t mx_scale = static_cast<uint32_t>((col >> 4) * (D / 2) + f_row * (D / 32));
+  auto mx_k = [&](int buf, int ks, int kt2) { return ld16(smem + buf * KBUF + mx_addr + kt2 * 16 * D + ks * 512); };
+  auto mx_ks = [&](int buf, int kt2) -> uint32_t {
+    const uint8_t* p = smem + SBASE + buf * SBUF + mx_scale + kt2 * D;
+    return (D == 128 ? *reinterpret_cast<const uint32_t*>(p) : *reinterpret_cast<const uint16_t*>(p)) >> (8 * half);
+  };
   // With PRE the K operands of the next tile are read into registers during the current tile's PV product.
   bf16x8 kop[KS][2];
+  uint4 kmx[KM][2];
+  uint32_t kmx_s[2];
   auto read_k = [&](int buf) {
+    if constexpr (FP4) {
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
+      for (int kt2 = 0; kt2 < 2; ++kt2) {
+        kmx_s[kt2] = mx_ks(buf, kt2);
 #pragma unroll
-      for (int kt2 = 0; kt2 < 2; ++kt2) kop[ks][kt2] = k_operand(buf, ks, kt2);
+        for (int ks = 0; ks < KM; ++ks) kmx[ks][kt2] = mx_k(buf, ks, kt2);
+      }
+    } else {
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int kt2 = 0; kt2 < 2; ++kt2) kop[ks][kt2] = k_operand(buf, ks, kt2);
+    }
   };
   if constexpr (PRE) read_k(0);
 
@@ -362,12 +399,30 @@ __device__ __forceinline__ void attn_fwd_block(const ExtendArgs& a, const int bl
     for (int kt2 = 0; kt2 < 2; ++kt2)
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[kt2][e] = 0.f;
+    if constexpr (FP4) {
+      if constexpr (!PRE) read_k(buf);
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
+      for (int kt2 = 0; kt2 < 2; ++kt2) s[kt2] = mx_score<0, 0>(kmx[0][kt2], kmx_s[kt2], query[0], s[kt2]);
 #pragma unroll
-      for (int kt2 = 0; kt2 < 2; ++kt2)
-        s[kt2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(PRE ? kop[ks][kt2] : k_operand(buf, ks, kt2), qop[ks], s[kt2],
-                                                         0, 0, 0);
+      for (int kt2 = 0; kt2 < 2; ++kt2) s[kt2] = mx_score<1, 0>(kmx[0][kt2], kmx_s[kt2], query[0], s[kt2]);
+#pragma unroll
+      for (int kt2 = 0; kt2 < 2; ++kt2) s[kt2] = mx_score<2, 0>(kmx[0][kt2], kmx_s[kt2], query[0], s[kt2]);
+      if constexpr (KM == 2) {
+#pragma unroll
+        for (int kt2 = 0; kt2 < 2; ++kt2) s[kt2] = mx_score<0, 2>(kmx[1][kt2], kmx_s[kt2], query[1], s[kt2]);
+#pragma unroll
+        for (int kt2 = 0; kt2 < 2; ++kt2) s[kt2] = mx_score<1, 2>(kmx[1][kt2], kmx_s[kt2], query[1], s[kt2]);
+#pragma unroll
+        for (int kt2 = 0; kt2 < 2; ++kt2) s[kt2] = mx_score<2, 2>(kmx[1][kt2], kmx_s[kt2], query[1], s[kt2]);
+      }
+    } else {
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int kt2 = 0; kt2 < 2; ++kt2)
+          s[kt2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(PRE ? kop[ks][kt2] : k_operand(buf, ks, kt2), qop[ks], s[kt2],
+                                                           0, 0, 0);
+    }
 
     bf16x8 vop[2][2][DT];
 #pragma unroll
@@ -539,7 +594,7 @@ __device__ __forceinline__ void attn_fwd_block(const ExtendArgs& a, const int bl
   // lanes: RPB rows of 2 D bytes) instead of 8 bytes in each of 32 rows (a 1437-token prompt 28.6 -> 25.9
   // us).
   constexpr int ORS = 2 * D + 16;
-  static_assert(NW * 32 * ORS <= 2 * NBUF * HALF_TILE, "the output rows of all waves fit the ring");
+  static_assert(NW * 32 * ORS <= LDS, "the output rows of all waves fit the ring");
   uint8_t* obuf = smem + wave * (32 * ORS);
   const float inv = 1.f / l_tot;
 #pragma unroll

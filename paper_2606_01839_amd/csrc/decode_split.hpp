@@ -92,15 +92,21 @@ __device__ __forceinline__ void split_body(const DecodeArgs& a, const int work, 
   const int c = lane & 15;   // MFMA column: query head within the group; A-operand row: key / dim
   const int qd = lane >> 4;  // k-block of the lane (8 consecutive k values)
 
-  // Query operand: head c of this kv head's group, dims 32*ks + 8*qd .. +8 (4-bit pages: (D/4) qd + 8 ks,
-  // so that a lane's K dims are consecutive).
+  // Query operand: head c of this kv head's group, dims 32*ks + 8*qd .. +8 (4-bit pages: (D/4) qd .. , the
+  // dims of K the lane holds).
   const int n_q_heads = a.n_kv_heads * a.group;
   bf16x8 qop[KS];
-  {
+  uint4 q4[4] = {};
+  if constexpr (FP4) {
+    const uint16_t* qrow = a.q + (static_cast<size_t>(dl * a.n_convs + conv_idx) * n_q_heads + g * a.group + c) * D + D / 4 * qd;
+#pragma unroll
+    for (int i = 0; i < KS; ++i)
+      if (c < a.group) q4[i] = ld16(qrow + 8 * i);
+  } else {
     const uint16_t* qrow = a.q + (static_cast<size_t>(dl * a.n_convs + conv_idx) * n_q_heads + g * a.group + c) * D;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
-      qop[ks] = c < a.group ? as_bf16x8(ld16(FP4 ? qrow + 8 * ks + D / 4 * qd : qrow + 32 * ks + 8 * qd)) : bf16x8{};
+      qop[ks] = c < a.group ? as_bf16x8(ld16(qrow + 32 * ks + 8 * qd)) : bf16x8{};
   }
 
   const int pid = lane < n_pg ? pt[lane] : 0;
@@ -116,37 +122,39 @@ __device__ __forceinline__ void split_body(const DecodeArgs& a, const int work, 
     const uint8_t* base = reinterpret_cast<const uint8_t*>(a.pool) + static_cast<size_t>(a.layer + dl) * a.n_pages * page_stride +
                           static_cast<size_t>(g) * B::kBytes;
     struct Page {
-      uint32_t k[NW], v[NW], ks, vs;
+      uint4 k;
+      uint32_t v[NW], ks, vs;
     };
     auto load = [&](int j) {
       Page p;
       const uint8_t* blk = base + static_cast<size_t>(__builtin_amdgcn_readlane(pid, j)) * page_stride;
       if constexpr (D == 128) {
-        const uint4 k = ld16_nt(blk + B::kK + 16 * lane), v = ld16_nt(blk + B::kV + 16 * lane);
-        p.k[0] = k.x, p.k[1] = k.y, p.k[2] = k.z, p.k[3] = k.w;
+        const uint4 v = ld16_nt(blk + B::kV + 16 * lane);
+        p.k = ld16_nt(blk + B::k_lane(lane));
         p.v[0] = v.x, p.v[1] = v.y, p.v[2] = v.z, p.v[3] = v.w;
       } else {
-        const uint2 k = ld8_nt(blk + B::kK + 8 * lane), v = ld8_nt(blk + B::kV + 8 * lane);
-        p.k[0] = k.x, p.k[1] = k.y;
+        const uint2 k = ld8_nt(blk + B::k_lane(lane)), v = ld8_nt(blk + B::kV + 8 * lane);
+        p.k = make_uint4(k.x, k.y, 0, 0);   // 16 of the instruction's 32 dims a lane
         p.v[0] = v.x, p.v[1] = v.y;
       }
-      p.ks = blk[B::k_scale(qd, c)];
+      p.ks = blk[B::k_scale_lane(lane)];
       p.vs = *reinterpret_cast<const uint32_t*>(blk + B::kVScale + 4 * qd);
       return p;
     };
     Page na = load(0), nb = load(n_pg > 1 ? 1 : 0);
+    const Bf6Query query = split_query(q4);
     for (int j = 0; j < n_pg; j += 2) {
       const Page pa = na, pb = nb;
       // the next page pair (the last one again at the end): its loads fly during this pair's arithmetic
       na = load(min(j + 2, n_pg - 1));
       nb = load(min(j + 3, n_pg - 1));
       f32x4 sa = {0.f, 0.f, 0.f, 0.f}, sb = {0.f, 0.f, 0.f, 0.f};
-      const float ksa = fp4_scale(pa.ks), ksb = fp4_scale(pb.ks);
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        sa = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(fp4_word(pa.k[ks], ksa)), qop[ks], sa, 0, 0, 0);
-        sb = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(fp4_word(pb.k[ks], ksb)), qop[ks], sb, 0, 0, 0);
-      }
+      sa = mx_score<0, 0>(pa.k, pa.ks, query, sa);
+      sb = mx_score<0, 0>(pb.k, pb.ks, query, sb);
+      sa = mx_score<1, 0>(pa.k, pa.ks, query, sa);
+      sb = mx_score<1, 0>(pb.k, pb.ks, query, sb);
+      sa = mx_score<2, 0>(pa.k, pa.ks, query, sa);
+      sb = mx_score<2, 0>(pb.k, pb.ks, query, sb);
       // sa[r]: head c, key k_begin + 16j + 4qd + r; sb[r]: the same + 16.
       const int key_a = k_begin + kPageTokens * j + 4 * qd;
       float x[8], vs[8];

@@ -189,7 +189,7 @@ __global__ __launch_bounds__(256) void kv_append_as_kernel(LaunchMeta, RopeArgs 
         const uint32_t codes = fp4_encode8(x, fp4_scale(kb));
         if (writes) {
           *reinterpret_cast<uint32_t*>(blk + B::k_word(t, ch)) = codes;
-          if ((ch & 3) == 0) blk[B::kKScale + (ch >> 2) * kPageTokens + t] = static_cast<uint8_t>(in ? kb : 0);
+          if ((ch & 3) == 0) blk[B::k_scale(t, ch >> 2)] = static_cast<uint8_t>(in ? kb : 0);
         }
         unpack8(vv[i][ps], x);
         const uint32_t vb = fp4_scale_byte(group_max<kCh>(max_bits(x)));
@@ -348,7 +348,7 @@ __global__ __launch_bounds__(256) void kv_read_kernel(LaunchMeta, const void* me
     if (t < c.t0 || t >= c.t1) continue;
     if constexpr (FP4)
       st16(k + at(t), fp4_word(*reinterpret_cast<const uint32_t*>(blk + B::k_word(t, ch)),
-                               fp4_scale(blk[B::kKScale + (ch >> 2) * kPageTokens + t])));
+                               fp4_scale(blk[B::k_scale(t, ch >> 2)])));
     else
       st16(k + at(t), ld16(blk16 + k_elem(t, ch)));
   }
@@ -368,11 +368,15 @@ __global__ __launch_bounds__(256) void kv_read_kernel(LaunchMeta, const void* me
 template <int D>
 __device__ __forceinline__ uint32_t fp4_mask_word(uint32_t x, int w, int valid) {
   using B = Fp4Block<D>;
-  if (4 * w < B::kV) return (w / B::kWords) % kPageTokens < valid ? x : 0u;
+  if (4 * w < B::kV) return (w / 4) % kPageTokens < valid ? x : 0u;
   if (4 * w < B::kKScale) return x & fp4_key_bits((w - B::kV / 4) / (16 * B::kWords), 0, valid);
-  const int t = (4 * w) % kPageTokens;   // the scales of four tokens (or padding)
   if (4 * w >= B::kPad) return 0u;
-  return valid >= t + 4 ? x : valid <= t ? 0u : x & ((1u << (8 * (valid - t))) - 1u);
+  // the scales of a token's K (D = 64: of two tokens'), or of four tokens' V
+  const bool is_v = 4 * w >= B::kVScale;
+  const int bytes = is_v ? 1 : D / 32;                                  // of a token
+  const int t = is_v ? 4 * w - B::kVScale : (4 * w - B::kKScale) / bytes;   // the first token
+  const int n = (valid - t) * bytes;                                    // bytes to keep
+  return n >= 4 ? x : n <= 0 ? 0u : x & ((1u << (8 * n)) - 1u);
 }
 
 template <int D>
@@ -484,14 +488,13 @@ __global__ __launch_bounds__(256) void kv_pack_fp4_kernel(const uint16_t* __rest
     vw[j] = fp4_encode8(x, 1.f);
   }
   if constexpr (D == 128) {
-    st16(dst + B::kK + 16 * lane, make_uint4(kw[0], kw[1], kw[2], kw[3]));
+    st16(dst + B::k_lane(lane), make_uint4(kw[0], kw[1], kw[2], kw[3]));
     st16(dst + B::kV + 16 * lane, make_uint4(vw[0], vw[1], vw[2], vw[3]));
-    dst[B::kKScale + lane] = static_cast<uint8_t>(c < valid ? kb : 0);
   } else {
-    st8(dst + B::kK + 8 * lane, make_uint2(kw[0], kw[1]));
+    st8(dst + B::k_lane(lane), make_uint2(kw[0], kw[1]));
     st8(dst + B::kV + 8 * lane, make_uint2(vw[0], vw[1]));
-    if ((qd & 1) == 0) dst[B::k_scale(qd, c)] = static_cast<uint8_t>(c < valid ? kb : 0);
   }
+  if (D == 128 || (qd & 1) == 0) dst[B::k_scale_lane(lane)] = static_cast<uint8_t>(c < valid ? kb : 0);
   if (c == 0) *reinterpret_cast<uint32_t*>(dst + B::kVScale + 4 * qd) = vb;
   if (lane < (B::kBytes - B::kPad) / 16) st16(dst + B::kPad + 16 * lane, make_uint4(0, 0, 0, 0));
 }

@@ -34,16 +34,16 @@ def test_encode_by_hand():
 def test_serialize_by_hand():
     d = 64
     k, v = np.zeros((1, 2, 1, d)), np.zeros((1, 2, 1, d))
-    k[0, 1, 0, 17] = 4.0      # token 1, part 1 (dims 16 .. 31), second code of the part
+    k[0, 1, 0, 49] = 4.0      # token 1, group 1 (dims 32 .. 63), its code 17: the second of byte 8
     v[0, 1, 0, 35] = -0.5     # dim 35 = 16 * 2 + 3: tile 2, row 3, token 1 of part 0
     w = o4.serialize(k, v)
     assert w.size == 17 * d
     want = np.zeros(17 * d, dtype=np.uint8)
-    want[(1 * 16 + 1) * 8] = 6 << 4                       # 4.0 with power 1
+    want[(1 * 16 + 1) * 16 + 8] = 6 << 4                  # 4.0 with power 1
     want[8 * d + (0 * 16 + 3) * 8 + 2 * 2] = 0xE << 4     # -0.5 = -4 x 2^-3
     ks = 16 * d
-    want[[ks, ks + 16, ks + 17]] = 1                      # groups of zeros: 2^-126
-    want[ks + 1] = 127
+    want[[ks, ks + 1, ks + 2]] = 1                        # groups of zeros: 2^-126
+    want[ks + 3] = 127
     want[ks + 32], want[ks + 33] = 1, 127 - 3
     assert w.tolist() == want.tolist()
 
