@@ -155,7 +155,7 @@ __device__ __forceinline__ void attn_fwd_block(const ExtendArgs& a, const int bl
   constexpr int SBASE = NBUF * KBUF, SBUF = FP4 ? 4 * D / 2 : 0;   // K scales of 4-bit pages after them
   constexpr int VBASE = SBASE + NBUF * SBUF;          // V^T parts after the K parts of all buffers
   constexpr int LDS = VBASE + NBUF * HALF_TILE;
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[LDS];
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[LDS + (FP4 ? 256 + (NBUF - 1) * SBUF : 0)];
 
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int tile_idx = block / a.n_kv_heads, g = block % a.n_kv_heads;
@@ -212,39 +212,45 @@ __device__ __forceinline__ void attn_fwd_block(const ExtendArgs& a, const int bl
     uint32_t k[NH], v[NH], ks, vs;
   };
   const int f_c = lane & 15, f_qd = lane >> 4, f_h = wave & 1;
-  const bool f_scales = lane < D / 16;    // lanes that take a word of the K scales
   const uint8_t* f_base = reinterpret_cast<const uint8_t*>(a.pool) +
                           (static_cast<size_t>(a.layer + dl) * a.n_pages * a.n_kv_heads + g) * B4::kBytes;
   const size_t f_stride = static_cast<size_t>(a.n_kv_heads) * B4::kBytes;
+  // Byte offsets in the block. The half's K scales are D / 16 words: the other lanes load one of them again.
+  const uint32_t f_k = B4::kK + f_h * 4 * D + lane * 4 * NH, f_v = B4::kV + (lane * B4::kWords + f_h * NH) * 4;
+  const uint32_t f_ks = B4::kKScale + f_h * (D / 4) + (lane % (D / 16)) * 4, f_vs = B4::kVScale + 4 * f_qd;
   auto load_codes = [&](int page) {
     Codes x;
     const uint8_t* blk = f_base + static_cast<size_t>(page) * f_stride;
-    const uint8_t* kc = blk + B4::kK + f_h * 4 * D + lane * 4 * NH;
-    const uint8_t* vc = blk + B4::kV + (lane * B4::kWords + f_h * NH) * 4;
     if constexpr (NH == 2) {
-      const uint2 kk = ld8(kc), vv = ld8(vc);
+      const uint2 kk = ld8(blk + f_k), vv = ld8(blk + f_v);
       x.k[0] = kk.x, x.k[1] = kk.y, x.v[0] = vv.x, x.v[1] = vv.y;
     } else {
-      x.k[0] = *reinterpret_cast<const uint32_t*>(kc);
-      x.v[0] = *reinterpret_cast<const uint32_t*>(vc);
+      x.k[0] = *reinterpret_cast<const uint32_t*>(blk + f_k);
+      x.v[0] = *reinterpret_cast<const uint32_t*>(blk + f_v);
     }
-    if (f_scales) x.ks = *reinterpret_cast<const uint32_t*>(blk + B4::kKScale + f_h * (D / 4) + lane * 4);
-    x.vs = *reinterpret_cast<const uint32_t*>(blk + B4::kVScale + 4 * f_qd);
+    x.ks = *reinterpret_cast<const uint32_t*>(blk + f_ks);
+    x.vs = *reinterpret_cast<const uint32_t*>(blk + f_vs);
     return x;
   };
-  // V^T dims 16 (2 NH f_h + t) + f_c, keys 4 f_qd .. + 3
-  const uint32_t f_v = static_cast<uint32_t>(q_w * (kPageTokens * 2 * D) + (32 * NH * f_h + f_c) * 32 +
-                                             (((f_qd >> 1) ^ ((f_c >> 2) & 1) ^ ((f_c >> 3) & 1)) * 16) + (f_qd & 1) * 8);
+  // LDS offsets: K codes; K scales (lanes without any write beside the ring); V^T, 16 bytes a lane: keys 8
+  // (f_qd / 2) .. + 7 of dims 16 (2 NH f_h + 2 i + f_qd % 2) + f_c, i = 0 .. NH - 1 (512 bytes further for 16 dims).
+  const uint32_t s_k = q_w * 8 * D + f_h * 4 * D + lane * 4 * NH;
+  const uint32_t s_ks = lane < D / 16 ? SBASE + q_w * (D / 2) + f_h * (D / 4) + lane * 4 : LDS + 4 * lane;
+  const uint32_t s_v = VBASE + q_w * (kPageTokens * 2 * D) + (32 * NH * f_h + 16 * (f_qd & 1) + f_c) * 32 +
+                       (((f_qd >> 1) ^ ((f_c >> 2) & 1) ^ ((f_c >> 3) & 1)) * 16);
   auto store_codes = [&](const Codes& x, int buf) {
-    uint8_t* kd = smem + buf * KBUF + q_w * 8 * D + f_h * 4 * D + lane * 4 * NH;
-    if constexpr (NH == 2) st8(kd, make_uint2(x.k[0], x.k[1]));
-    else *reinterpret_cast<uint32_t*>(kd) = x.k[0];
-    if (f_scales) *reinterpret_cast<uint32_t*>(smem + SBASE + buf * SBUF + q_w * (D / 2) + f_h * (D / 4) + lane * 4) = x.ks;
-    const float vs[4] = {fp4_scale_of(x.vs, 0), fp4_scale_of(x.vs, 1), fp4_scale_of(x.vs, 2), fp4_scale_of(x.vs, 3)};
+    if constexpr (NH == 2) st8(smem + s_k + buf * KBUF, make_uint2(x.k[0], x.k[1]));
+    else *reinterpret_cast<uint32_t*>(smem + s_k + buf * KBUF) = x.k[0];
+    *reinterpret_cast<uint32_t*>(smem + s_ks + buf * SBUF) = x.ks;
+    const float vs[4] = {fp4_exponent_of(x.vs, 0), fp4_exponent_of(x.vs, 1), fp4_exponent_of(x.vs, 2), fp4_exponent_of(x.vs, 3)};
 #pragma unroll
-    for (int i = 0; i < NH; ++i) {   // (16 dims on: 512 bytes; bits 2 and 3 of the dim are f_c's)
-      st8(smem + VBASE + buf * HALF_TILE + f_v + (2 * i) * 512, fp4_quad<0>(x.v[i], vs));
-      st8(smem + VBASE + buf * HALF_TILE + f_v + (2 * i + 1) * 512, fp4_quad<1>(x.v[i], vs));
+    for (int i = 0; i < NH; ++i) {
+      // Lane rows f_qd and f_qd ^ 1 hold four keys each of two dim tiles and exchange, so that each has the
+      // eight keys of one and writes 16 bytes (8-byte writes of 16 lanes meet in pairs of banks).
+      const uint2 t0 = fp4_quad<0>(x.v[i], vs), t1 = fp4_quad<1>(x.v[i], vs);
+      const auto lo = __builtin_amdgcn_permlane16_swap(t0.x, t1.x, false, false);
+      const auto hi = __builtin_amdgcn_permlane16_swap(t0.y, t1.y, false, false);
+      st16(smem + s_v + buf * HALF_TILE + 2 * i * 512, make_uint4(lo[0], hi[0], lo[1], hi[1]));
     }
   };
   Codes codes{};   // of the tile after the next
@@ -393,7 +399,7 @@ __device__ __forceinline__ void attn_fwd_block(const ExtendArgs& a, const int bl
   if constexpr (PRE) read_k(0);
 
   auto tile_step = [&](const int j, const int buf) {
-    feed(buf);
+    if constexpr (!FP4) feed(buf);
     f32x16 s[2];
 #pragma unroll
     for (int kt2 = 0; kt2 < 2; ++kt2)
@@ -414,6 +420,13 @@ __device__ __forceinline__ void attn_fwd_block(const ExtendArgs& a, const int bl
         for (int kt2 = 0; kt2 < 2; ++kt2) s[kt2] = mx_score<1, 2>(kmx[1][kt2], kmx_s[kt2], query[1], s[kt2]);
 #pragma unroll
         for (int kt2 = 0; kt2 < 2; ++kt2) s[kt2] = mx_score<2, 2>(kmx[1][kt2], kmx_s[kt2], query[1], s[kt2]);
+      }
+      // the conversion of tile j+2 goes between the score products, which leave the vector units free
+      feed(buf);
+#pragma unroll
+      for (int i = 0; i < 6 * KM; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
       }
     } else {
 #pragma unroll

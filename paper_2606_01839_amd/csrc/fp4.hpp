@@ -56,6 +56,11 @@ __device__ __forceinline__ float fp4_scale_of(uint32_t w, int b) {
   return __uint_as_float(b == 0 ? (w << 23) & 0x7F800000u : (w >> (8 * b)) << 23 & 0x7F800000u);
 }
 
+// the same for the conversion instructions, which look at a scale's exponent bits only
+__device__ __forceinline__ float fp4_exponent_of(uint32_t w, int b) {
+  return __uint_as_float(b == 0 ? w << 23 : b == 1 ? w << 15 : b == 2 ? w << 7 : w >> 1);
+}
+
 // Two codes (byte B of w) as bf16 values times a power of two (v_cvt_scalef32_pk_bf16_fp4; it uses the
 // scale's exponent only). Exact.
 template <int B>
