@@ -240,6 +240,8 @@ class KVPool:
         self.desc = PoolDesc(n_layers, n_q_heads, n_kv_heads, head_dim, max_convs,
                              max_pages_per_conv, n_pages)
         self.device = torch.device(device)
+        # what Tensor.get_device() gives for tensors of this device (a comparison of devices costs 1 us a call)
+        self._index = -1 if self.device.type == "cpu" else self.device.index or 0
         self.n_layers, self.n_q_heads, self.n_kv_heads, self.head_dim = (
             n_layers, n_q_heads, n_kv_heads, head_dim)
         kvb = self.lib.cs_pool_kv_bytes_as(ctypes.byref(self.desc), fmt)
@@ -322,8 +324,7 @@ class KVPool:
     def _dev(self, t: torch.Tensor, name: str, shape=None) -> int:
         if t.dtype != torch.bfloat16:
             raise ValueError(f"{name} must be bfloat16, got {t.dtype}")
-        if t.device != self.device and not (t.device.type == self.device.type == "cuda"
-                                            and (t.device.index or 0) == (self.device.index or 0)):
+        if t.get_device() != self._index or t.is_cuda != (self._index >= 0):
             raise ValueError(f"{name} must be on {self.device}, got {t.device}")
         if not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous")
@@ -365,7 +366,7 @@ class KVPool:
             qshp = (self.n_layers, sum(na), self.n_q_heads, self.head_dim)
             qp = self._dev(q, "q", qshp)
             if q_out is None:
-                q_out = torch.empty(qshp, dtype=torch.bfloat16, device=self.device)
+                q_out = torch.empty_like(q)
             op = self._rotated(q, q_out, "q_out", qshp)
         elif q_out is not None:
             raise ValueError("q_out without q")
@@ -385,8 +386,10 @@ class KVPool:
             shp = (q.shape[0],) + shp
         qp = self._dev(q, "q", shp)
         if out is None:
-            out = torch.empty(shp, dtype=torch.bfloat16, device=self.device)
-        op = self._rotated(q, out, "out", shp)
+            out = torch.empty_like(q)
+            op = out.data_ptr()
+        else:
+            op = self._rotated(q, out, "out", shp)
         _check(self.lib.cs_rope_q(self._handle, ctypes.byref(rope.desc), len(ca), cp, qlp, shp[0] if len(shp) == 4 else 1, qp, op,
                                   _stream_handle(self.device)))
         return out
@@ -409,7 +412,10 @@ class KVPool:
         shp = (self.n_layers, sum(na), self.n_kv_heads, self.head_dim)
         if min(na, default=0) < 0:
             raise ValueError("lens must not be negative")
-        k, v = (torch.empty(shp, dtype=torch.bfloat16, device=self.device) if x is None else x for x in (k, v))
+        if k is None:
+            k = torch.empty(shp, dtype=torch.bfloat16, device=self.device)
+        if v is None:
+            v = torch.empty_like(k)
         kp, vp = self._dev(k, "k", shp), self._dev(v, "v", shp)
         _check(self.lib.cs_kv_read(self._handle, len(ca), cp, sa.buffer_info()[0], npp, kp, vp, _stream_handle(self.device)))
         return k, v
@@ -423,8 +429,10 @@ class KVPool:
         shp = (sum(qa), self.n_q_heads, self.head_dim)
         qptr = self._dev(q, "q", shp)
         if out is None:
-            out = torch.empty(shp, dtype=torch.bfloat16, device=self.device)
-        optr = self._dev(out, "out", shp)
+            out = torch.empty_like(q)
+            optr = out.data_ptr()
+        else:
+            optr = self._dev(out, "out", shp)
         _check(fn(self._handle, len(ca), cp, qp, layer, qptr, optr, _stream_handle(self.device)))
         return out
 
@@ -446,8 +454,10 @@ class KVPool:
         shp = (len(ca), self.n_q_heads, self.head_dim)
         qptr = self._dev(q, "q", shp)
         if out is None:
-            out = torch.empty(shp, dtype=torch.bfloat16, device=self.device)
-        optr = self._dev(out, "out", shp)
+            out = torch.empty_like(q)
+            optr = out.data_ptr()
+        else:
+            optr = self._dev(out, "out", shp)
         _check(fn(self._handle, len(ca), cp, layer, qptr, optr, _stream_handle(self.device)))
         return out
 
