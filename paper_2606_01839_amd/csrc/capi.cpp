@@ -653,6 +653,30 @@ struct RotatedAppend {
   void* q_out = nullptr;
 };
 
+// Queries [n_layers][rows][n_q_heads][head_dim] rotated in launches of their own.
+cs_status run_rope_q(cs_pool* p, const std::vector<cs::RopeConv>& convs, int64_t rows, int32_t n_layers, const cs::RopeArgs& rope,
+                     const void* q, void* out) {
+  Blob b;
+  b.push(convs.data(), convs.size());
+  if (b.bytes.size() > kQuarter) return fail(CS_ENOMEM, "batch descriptor exceeds the metadata ring");
+  cs::Meta m;
+  cs_status st = place_meta(p, b, &m);
+  const cs::PoolGeom g = p->geom();
+  const size_t layer_bytes = static_cast<size_t>(rows) * g.n_q_heads * g.head_dim * 2;
+  const int per = cs::rope_q_layers(g);   // of one launch
+  for (int32_t l = 0; l < n_layers && st == CS_OK; l += per)
+    st = timed_launch(p, CS_PROF_APPEND, "query rotation launch", [&] {
+      return cs::launch_rope_q(g, m, static_cast<int>(convs.size()), rows, std::min(per, n_layers - l), rope,
+                               static_cast<const char*>(q) + l * layer_bytes, static_cast<char*>(out) + l * layer_bytes, p->stream);
+    });
+  return st;
+}
+
+// An append rotates more query bytes than this in a launch of their own (5300 tokens, 32 layers, 32 query heads,
+// 1.4 GB: 764 us in two launches, 803 in one, whose workgroups of queries share a CU with the LDS of the K and
+// V's); below, one launch saves the other's start (64 single tokens of 32 layers, 17 MB).
+constexpr size_t kRopeApartBytes = size_t(64) << 20;
+
 // `rotated` (may be null): keys turn on their way into the pages, and the queries with them.
 cs_status append_impl(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t* n_new,
                       const void* k, const void* v, cs_stream stream, const Blob* carry = nullptr,
@@ -698,10 +722,13 @@ cs_status append_impl(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t
 
   const cs::PoolGeom g = p->geom();
   const size_t carry_bytes = carry ? carry->bytes.size() : 0;
+  const bool q_apart = rotated && rotated->q &&
+                       static_cast<size_t>(total) * g.n_layers * g.n_q_heads * g.head_dim * 2 > kRopeApartBytes;
   auto launch = [&](const cs::Meta& m, int n_chunks, const cs::AppendCarry& c) {
     return timed_launch(p, CS_PROF_APPEND, "append launch", [&] {
       if (rotated)
-        return cs::launch_append_as(g, m, n_chunks, c, &rotated->rope, k, v, rotated->q, rotated->q_out, total, p->stream);
+        return cs::launch_append_as(g, m, n_chunks, c, &rotated->rope, k, v, q_apart ? nullptr : rotated->q, rotated->q_out, total,
+                                    p->stream);
       if (p->fp4) return cs::launch_append_as(g, m, n_chunks, c, nullptr, k, v, nullptr, nullptr, total, p->stream);
       return cs::launch_append(g, m, n_chunks, c, k, v, total, p->stream);
     });
@@ -736,6 +763,15 @@ cs_status append_impl(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t
     // After the chunks, which may go round the ring: nothing of it is reused before the launches that read
     // the carried metadata are issued.
     if (carry_bytes > 0 && st == CS_OK) st = upload(p, carry->bytes.data(), carry_bytes, carry_dev);
+  }
+  if (q_apart && st == CS_OK) {
+    std::vector<cs::RopeConv> rc;
+    int32_t row = 0;
+    for (int32_t i = 0; i < n; ++i) {
+      if (nn[i] > 0) rc.push_back({row, static_cast<int32_t>(old_lens[i])});
+      row += nn[i];
+    }
+    st = run_rope_q(p, rc, total, g.n_layers, rotated->rope, rotated->q, rotated->q_out);
   }
   if (st != CS_OK) {
     roll_back();
@@ -927,22 +963,9 @@ cs_status cs_rope_q(cs_pool* p, const cs_rope* rope, int32_t n, const cs_conv* c
   }
   if (rows == 0 || n_layers == 0) return CS_OK;
   if (!q || !out) return fail(CS_EINVAL, "null q/out");
-  Blob b;
-  b.push(rc.data(), rc.size());
-  if (b.bytes.size() > kQuarter) return fail(CS_ENOMEM, "batch descriptor exceeds the metadata ring");
   if ((st = ensure_device(p)) != CS_OK) return st;
   if ((st = use_stream(p, as_stream(stream))) != CS_OK) return st;
-  cs::Meta m;
-  if ((st = place_meta(p, b, &m)) != CS_OK) return st;
-  const cs::PoolGeom g = p->geom();
-  const size_t layer_bytes = static_cast<size_t>(rows) * g.n_q_heads * g.head_dim * 2;
-  const int per = cs::rope_q_layers(g);   // of one launch
-  for (int32_t l = 0; l < n_layers && st == CS_OK; l += per)
-    st = timed_launch(p, CS_PROF_APPEND, "query rotation launch", [&] {
-      return cs::launch_rope_q(g, m, static_cast<int>(rc.size()), rows, std::min(per, n_layers - l), r,
-                               static_cast<const char*>(q) + l * layer_bytes, static_cast<char*>(out) + l * layer_bytes, p->stream);
-    });
-  return st;
+  return run_rope_q(p, rc, rows, n_layers, r, q, out);
 }
 
 cs_status cs_kv_read(cs_pool* p, int32_t n, const cs_conv* convs, const int64_t* starts, const int32_t* counts, void* k, void* v,

@@ -140,7 +140,7 @@ __global__ __launch_bounds__(256) void kv_append_as_kernel(LaunchMeta, RopeArgs 
           float f[8];
           unpack8(x[i][ps], f);
           rope_rotate<D>(f, ch, rope, tab[i * kPageTokens + t]);
-          if (have[i] && t >= c[i].t0 && t < c[i].t1) st16(a.q_out + row_at(layer, i, t, a.n_q_heads, h), pack8(f));
+          if (have[i] && t >= c[i].t0 && t < c[i].t1) st16_nt(a.q_out + row_at(layer, i, t, a.n_q_heads, h), pack8(f));
         }
     }
     return;
@@ -158,8 +158,8 @@ __global__ __launch_bounds__(256) void kv_append_as_kernel(LaunchMeta, RopeArgs 
       kv[i][ps] = vv[i][ps] = make_uint4(0, 0, 0, 0);
       if (have[i] && t >= c[i].t0 && t < c[i].t1) {
         const size_t src = row_at(layer, i, t, a.n_kv_heads, head);
-        kv[i][ps] = ld16(a.k + src);
-        vv[i][ps] = ld16(a.v + src);
+        kv[i][ps] = FP4 ? ld16_nt(a.k + src) : ld16(a.k + src);
+        vv[i][ps] = FP4 ? ld16_nt(a.v + src) : ld16(a.v + src);
       }
     }
   if constexpr (ROPE) rope_table<D>(tab, CH * kPageTokens, rope, waves, row_pos);
@@ -228,7 +228,7 @@ __global__ __launch_bounds__(256) void kv_append_as_kernel(LaunchMeta, RopeArgs 
 #pragma unroll
           for (int j = 0; j < B::kWords; ++j) w[j] = (dst[j] & ~keep) | (w[j] & keep);
         }
-        if constexpr (D == 128) st16(dst, make_uint4(w[0], w[1], w[2], w[3]));
+        if constexpr (D == 128) st16_nt(dst, make_uint4(w[0], w[1], w[2], w[3]));
         else st8(dst, make_uint2(w[0], w[1]));
       }
     } else {
@@ -255,9 +255,14 @@ __global__ __launch_bounds__(256) void kv_append_as_kernel(LaunchMeta, RopeArgs 
 }
 
 // ---------------------------------------------------------------------------------------------
-// Queries rotated at their positions: 16 rows and kQHeads heads per workgroup.
+// Queries rotated at their positions: 16 rows and kQHeads heads per workgroup. Bound by HBM: 5.69 TB/s read and
+// written over 1.4 GB of queries (a copy: 5.76). NT: streaming loads, for queries that the last-level cache (256 MB)
+// cannot hold beside the output: 1.4 GB 488 us against 505 with plain loads, but 131 MB that a kernel before has just written
+// 50.6 against 44.8.
 // ---------------------------------------------------------------------------------------------
-template <int D>
+constexpr size_t kRopeStreamBytes = size_t(128) << 20;
+
+template <int D, bool NT>
 __global__ __launch_bounds__(256) void rope_q_kernel(LaunchMeta, RopeArgs rope, const void* meta, int n_convs, int64_t rows,
                                                      int n_q_heads, int q_groups, const uint16_t* q,
                                                      uint16_t* out) {
@@ -284,7 +289,8 @@ __global__ __launch_bounds__(256) void rope_q_kernel(LaunchMeta, RopeArgs rope, 
 #pragma unroll
     for (int ps = 0; ps < kPasses; ++ps) {
       const int t = t_lane + ps * kRows;
-      x[ps] = row0 + t < rows ? ld16(q + at(t)) : make_uint4(0, 0, 0, 0);
+      x[ps] = make_uint4(0, 0, 0, 0);
+      if (row0 + t < rows) x[ps] = NT ? ld16_nt(q + at(t)) : ld16(q + at(t));
     }
 #pragma unroll
     for (int ps = 0; ps < kPasses; ++ps) {
@@ -292,7 +298,7 @@ __global__ __launch_bounds__(256) void rope_q_kernel(LaunchMeta, RopeArgs rope, 
       float f[8];
       unpack8(x[ps], f);
       rope_rotate<D>(f, ch, rope, tab[t]);
-      if (row0 + t < rows) st16(out + at(t), pack8(f));
+      if (row0 + t < rows) st16_nt(out + at(t), pack8(f));
     }
   }
 }
@@ -347,16 +353,16 @@ __global__ __launch_bounds__(256) void kv_read_kernel(LaunchMeta, const void* me
     const int t = t_lane + ps * kRows;
     if (t < c.t0 || t >= c.t1) continue;
     if constexpr (FP4)
-      st16(k + at(t), fp4_word(*reinterpret_cast<const uint32_t*>(blk + B::k_word(t, ch)),
+      st16_nt(k + at(t), fp4_word(*reinterpret_cast<const uint32_t*>(blk + B::k_word(t, ch)),
                                fp4_scale(blk[B::k_scale(t, ch >> 2)])));
     else
-      st16(k + at(t), ld16(blk16 + k_elem(t, ch)));
+      st16_nt(k + at(t), ld16(blk16 + k_elem(t, ch)));
   }
   __syncthreads();
 #pragma unroll
   for (int ps = 0; ps < kPasses; ++ps) {
     const int t = t_lane + ps * kRows;
-    if (t >= c.t0 && t < c.t1) st16(v + at(t), ld16(vt + t * kStride + ch * 8));
+    if (t >= c.t0 && t < c.t1) st16_nt(v + at(t), ld16(vt + t * kStride + ch * 8));
   }
 }
 
@@ -566,9 +572,13 @@ hipError_t launch_rope_q(const PoolGeom& g, const Meta& meta, int n_convs, int64
   const dim3 grid(static_cast<unsigned>((rows + kPageTokens - 1) / kPageTokens), n_layers * q_groups);
   return by_dim(g.head_dim, [&](auto dc) {
     constexpr int D = decltype(dc)::value;
-    rope_q_kernel<D><<<grid, 256, 0, stream>>>(m, rope, meta.dev, n_convs, rows, g.n_q_heads, q_groups,
-                                               static_cast<const uint16_t*>(q), static_cast<uint16_t*>(out));
-    return hipGetLastError();
+    auto launch = [&](auto kernel) {
+      kernel<<<grid, 256, 0, stream>>>(m, rope, meta.dev, n_convs, rows, g.n_q_heads, q_groups,
+                                       static_cast<const uint16_t*>(q), static_cast<uint16_t*>(out));
+      return hipGetLastError();
+    };
+    const size_t bytes = static_cast<size_t>(rows) * n_layers * g.n_q_heads * D * 2;
+    return bytes > kRopeStreamBytes ? launch(rope_q_kernel<D, true>) : launch(rope_q_kernel<D, false>);
   });
 }
 
