@@ -64,7 +64,7 @@ __global__ __launch_bounds__(kDecodeItemThreads) void decode_split_kernel(Launch
 
 // the same over 4-bit pages
 template <int D>
-__global__ __launch_bounds__(kDecodeItemThreads) void decode_split_fp4_kernel(LaunchMeta, DecodeArgs a) {
+__global__ __launch_bounds__(kDecodeItemThreads) __attribute__((amdgpu_waves_per_eu(4))) void decode_split_fp4_kernel(LaunchMeta, DecodeArgs a) {
   __shared__ float xch[split_exchange_floats<D>()];
   split_body<D, true>(a, blockIdx.x, blockIdx.y, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), xch);
 }

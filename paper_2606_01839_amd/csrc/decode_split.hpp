@@ -2,6 +2,7 @@
 // decode kernels and by the fused extend + decode kernels of a mixed step; see decode.hip.
 #pragma once
 
+#include <cfloat>
 #include <cmath>
 
 #include "device_common.hpp"
@@ -116,6 +117,7 @@ __device__ __forceinline__ void split_body(const DecodeArgs& a, const int work, 
   for (int t = 0; t < DT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 
   if constexpr (FP4) {
+    const bf16x2 ones = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
     using B = Fp4Block<D>;
     constexpr int NW = B::kWords;
     const size_t page_stride = static_cast<size_t>(a.n_kv_heads) * B::kBytes;
@@ -141,13 +143,8 @@ __device__ __forceinline__ void split_body(const DecodeArgs& a, const int work, 
       p.vs = *reinterpret_cast<const uint32_t*>(blk + B::kVScale + 4 * qd);
       return p;
     };
-    Page na = load(0), nb = load(n_pg > 1 ? 1 : 0);
-    const Bf6Query query = split_query(q4);
-    for (int j = 0; j < n_pg; j += 2) {
-      const Page pa = na, pb = nb;
-      // the next page pair (the last one again at the end): its loads fly during this pair's arithmetic
-      na = load(min(j + 2, n_pg - 1));
-      nb = load(min(j + 3, n_pg - 1));
+    // Keys of the page pair j, j + 1 (a last single page stands in for its second).
+    auto step = [&](const Page& pa, const Page& pb, const int j, const Bf6Query& query) {
       f32x4 sa = {0.f, 0.f, 0.f, 0.f}, sb = {0.f, 0.f, 0.f, 0.f};
       sa = mx_score<0, 0>(pa.k, pa.ks, query, sa);
       sb = mx_score<0, 0>(pb.k, pb.ks, query, sb);
@@ -156,17 +153,12 @@ __device__ __forceinline__ void split_body(const DecodeArgs& a, const int work, 
       sa = mx_score<2, 0>(pa.k, pa.ks, query, sa);
       sb = mx_score<2, 0>(pb.k, pb.ks, query, sb);
       // sa[r]: head c, key k_begin + 16j + 4qd + r; sb[r]: the same + 16.
-      const int key_a = k_begin + kPageTokens * j + 4 * qd;
-      float x[8], vs[8];
+      float x[8] = {sa[0], sa[1], sa[2], sa[3], sb[0], sb[1], sb[2], sb[3]}, vs[8];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        x[r] = sa[r] * a.scale_log2;
-        x[4 + r] = sb[r] * a.scale_log2;
-        vs[r] = fp4_scale_of(pa.vs, r);
-        vs[4 + r] = fp4_scale_of(pb.vs, r);
-      }
+      for (int r = 0; r < 8; ++r) vs[r] = fp4_scale_of(r < 4 ? pa.vs : pb.vs, r % 4);
       if (k_begin + kPageTokens * (j + 2) > k_end) {
         // keys past the wave's range: weight 0, and 0 for the scale too (0 x a scale of 255 would be NaN)
+        const int key_a = k_begin + kPageTokens * j + 4 * qd;
 #pragma unroll
         for (int r = 0; r < 8; ++r) {
           const bool in = key_a + (r < 4 ? r : kPageTokens + r - 4) < k_end;
@@ -174,24 +166,40 @@ __device__ __forceinline__ void split_body(const DecodeArgs& a, const int work, 
           vs[r] = in ? vs[r] : 0.f;
         }
       }
-      float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-      mx = fmaxf(mx, xor_shfl(mx, 16));
-      mx = fmaxf(mx, xor_shfl(mx, 32));
-      const float m_new = fmaxf(m_run, mx);
-      if (__builtin_amdgcn_ballot_w64(m_new > m_run) != 0) {
+      // Weights against the running maximum, which is refreshed only where a lane's sum exceeds 2^8 or is not
+      // finite (always in the first step), as in the attention kernel: no maximum and no exchange between
+      // lanes on the common path.
+      float p[8];
+      uint4 pw;
+      auto weights = [&] {
+        float ps0 = 0.f, ps1 = 0.f;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) p[r] = fast_exp2(__builtin_fmaf(x[r], a.scale_log2, -m_run));
+        pw = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
+        // The denominator sums the same bf16-rounded weights the PV product uses: scaling by the values' power
+        // of two commutes with the rounding.
+        ps0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pw.x), ones, ps0, false);
+        ps1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pw.y), ones, ps1, false);
+        ps0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pw.z), ones, ps0, false);
+        ps1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pw.w), ones, ps1, false);
+        return ps0 + ps1;
+      };
+      float ps = weights();
+      if (__builtin_amdgcn_ballot_w64(!(ps <= 256.f)) != 0) {
+        float mx = x[0];
+#pragma unroll
+        for (int r = 1; r < 8; ++r) mx = fmaxf(mx, x[r]);
+        mx = fmaxf(mx, xor_shfl(mx, 16));
+        mx = fmaxf(mx, xor_shfl(mx, 32));
+        const float m_new = fmaxf(m_run, mx * a.scale_log2);
         const float alpha = fast_exp2(m_run - m_new);
+        m_run = m_new;
         l_run *= alpha;
 #pragma unroll
         for (int t = 0; t < DT; ++t) o[t] *= alpha;
-        m_run = m_new;
+        ps = weights();
       }
-      float p[8];
-#pragma unroll
-      for (int r = 0; r < 8; ++r) p[r] = fast_exp2(x[r] - m_run);
-      const uint4 pw = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
-      // The denominator sums the same bf16-rounded weights the PV product uses: scaling by the values' power
-      // of two commutes with the rounding.
-      l_run += (sum_bf16x2(pw.x) + sum_bf16x2(pw.y)) + (sum_bf16x2(pw.z) + sum_bf16x2(pw.w));
+      l_run += ps;
       const bf16x8 pop = as_bf16x8(make_uint4(pack_bf16x2(p[0] * vs[0], p[1] * vs[1]), pack_bf16x2(p[2] * vs[2], p[3] * vs[3]),
                                               pack_bf16x2(p[4] * vs[4], p[5] * vs[5]), pack_bf16x2(p[6] * vs[6], p[7] * vs[7])));
 #pragma unroll
@@ -202,6 +210,29 @@ __device__ __forceinline__ void split_body(const DecodeArgs& a, const int work, 
         o[2 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
             as_bf16x8(make_uint2(fp4_pair<2>(pa.v[w], 1.f), fp4_pair<3>(pa.v[w], 1.f)),
                       make_uint2(fp4_pair<2>(pb.v[w], 1.f), fp4_pair<3>(pb.v[w], 1.f))), pop, o[2 * w + 1], 0, 0, 0);
+      }
+    };
+    m_run = -FLT_MAX;   // (a wave without keys keeps it: its weight in the merge is 0)
+    // The next page pair's loads fly during this one's arithmetic (past the end the last page is loaded again). Head
+    // dim 64 takes two pairs in turn, without copies; at 128 a second set of registers would leave one workgroup a
+    // CU (decode of 64 conversations of 8k-32k tokens 208 -> 220 us).
+    Page a0 = load(0), b0 = load(min(1, max(n_pg - 1, 0)));
+    const Bf6Query query = split_query(q4);
+    if constexpr (D == 64) {
+      for (int j = 0; j < n_pg; j += 4) {
+        const Page a1 = load(min(j + 2, n_pg - 1)), b1 = load(min(j + 3, n_pg - 1));
+        step(a0, b0, j, query);
+        if (j + 2 >= n_pg) break;
+        a0 = load(min(j + 4, n_pg - 1));
+        b0 = load(min(j + 5, n_pg - 1));
+        step(a1, b1, j + 2, query);
+      }
+    } else {
+      for (int j = 0; j < n_pg; j += 2) {
+        const Page pa = a0, pb = b0;
+        a0 = load(min(j + 2, n_pg - 1));
+        b0 = load(min(j + 3, n_pg - 1));
+        step(pa, pb, j, query);
       }
     }
   } else {

@@ -53,7 +53,7 @@ __device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x
 __device__ __forceinline__ float fp4_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
 // byte b of w as such a scale
 __device__ __forceinline__ float fp4_scale_of(uint32_t w, int b) {
-  return __uint_as_float(b == 0 ? (w << 23) & 0x7F800000u : (w >> (8 * b)) << 23 & 0x7F800000u);
+  return __uint_as_float(((w >> (8 * b)) & 0xFFu) << 23);
 }
 
 // the same for the conversion instructions, which look at a scale's exponent bits only
@@ -132,36 +132,32 @@ __device__ __forceinline__ f32x32 from_bf6(u32x6 x, float scale) {
 }
 
 __device__ __forceinline__ Bf6Query split_query(const uint4 (&x)[4]) {
-  float v[32];
+  f32x16 even, odd;
   uint32_t m = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      v[8 * i + 2 * j] = bf16_lo(w[j]);
-      v[8 * i + 2 * j + 1] = bf16_hi(w[j]);
+      even[4 * i + j] = bf16_lo(w[j]);
+      odd[4 * i + j] = bf16_hi(w[j]);
+      m = max(m, max(abs_bits(bf16_lo(w[j])), abs_bits(bf16_hi(w[j]))));
     }
   }
-#pragma unroll
-  for (int i = 0; i < 32; ++i) m = max(m, abs_bits(v[i]));
   const uint32_t top = max(m >> 23, 10u);   // at least 2^-117: smaller queries lose bits of scores below 2^-100
   Bf6Query q;
   q.scale = (top - 3) | (top - 6) << 8 | (top - 9) << 16;
 #pragma unroll
   for (int k = 0; k < 3; ++k) {
     const float s = fp4_scale(top - 3 - 3 * k);
-    f32x16 even, odd;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      even[i] = v[2 * i];
-      odd[i] = v[2 * i + 1];
-    }
     q.p[k] = to_bf6(even, odd, s);
     if (k == 2) break;
     const f32x32 back = from_bf6(q.p[k], s);
 #pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] -= back[i];
+    for (int i = 0; i < 16; ++i) {
+      even[i] -= back[2 * i];
+      odd[i] -= back[2 * i + 1];
+    }
   }
   return q;
 }
