@@ -221,15 +221,18 @@ __device__ __forceinline__ void attn_fwd_block(const ExtendArgs& a, const int bl
   auto load_codes = [&](int page) {
     Codes x;
     const uint8_t* blk = f_base + static_cast<size_t>(page) * f_stride;
+    // (as 32-bit offsets to a scalar base; hoisted out of the loop they would be widened to register pairs)
+    uint32_t ok = f_k, ov = f_v, oks = f_ks, ovs = f_vs;
+    asm volatile("" : "+v"(ok), "+v"(ov), "+v"(oks), "+v"(ovs));
     if constexpr (NH == 2) {
-      const uint2 kk = ld8(blk + f_k), vv = ld8(blk + f_v);
+      const uint2 kk = ld8(blk + ok), vv = ld8(blk + ov);
       x.k[0] = kk.x, x.k[1] = kk.y, x.v[0] = vv.x, x.v[1] = vv.y;
     } else {
-      x.k[0] = *reinterpret_cast<const uint32_t*>(blk + f_k);
-      x.v[0] = *reinterpret_cast<const uint32_t*>(blk + f_v);
+      x.k[0] = *reinterpret_cast<const uint32_t*>(blk + ok);
+      x.v[0] = *reinterpret_cast<const uint32_t*>(blk + ov);
     }
-    x.ks = *reinterpret_cast<const uint32_t*>(blk + f_ks);
-    x.vs = *reinterpret_cast<const uint32_t*>(blk + f_vs);
+    x.ks = *reinterpret_cast<const uint32_t*>(blk + oks);
+    x.vs = *reinterpret_cast<const uint32_t*>(blk + ovs);
     return x;
   };
   // LDS offsets: K codes; K scales (lanes without any write beside the ring); V^T, 16 bytes a lane: keys 8

@@ -127,20 +127,24 @@ __device__ __forceinline__ void split_body(const DecodeArgs& a, const int work, 
       uint4 k;
       uint32_t v[NW], ks, vs;
     };
+    const uint32_t f_k = B::k_lane(lane), f_v = B::kV + lane * 4 * NW, f_ks = B::k_scale_lane(lane), f_vs = B::kVScale + 4 * qd;
     auto load = [&](int j) {
       Page p;
       const uint8_t* blk = base + static_cast<size_t>(__builtin_amdgcn_readlane(pid, j)) * page_stride;
+      // (as 32-bit offsets to a scalar base; hoisted out of the loop they would be widened to register pairs)
+      uint32_t ok = f_k, ov = f_v, oks = f_ks, ovs = f_vs;
+      asm volatile("" : "+v"(ok), "+v"(ov), "+v"(oks), "+v"(ovs));
       if constexpr (D == 128) {
-        const uint4 v = ld16_nt(blk + B::kV + 16 * lane);
-        p.k = ld16_nt(blk + B::k_lane(lane));
+        const uint4 v = ld16_nt(blk + ov);
+        p.k = ld16_nt(blk + ok);
         p.v[0] = v.x, p.v[1] = v.y, p.v[2] = v.z, p.v[3] = v.w;
       } else {
-        const uint2 k = ld8_nt(blk + B::k_lane(lane)), v = ld8_nt(blk + B::kV + 8 * lane);
+        const uint2 k = ld8_nt(blk + ok), v = ld8_nt(blk + ov);
         p.k = make_uint4(k.x, k.y, 0, 0);   // 16 of the instruction's 32 dims a lane
         p.v[0] = v.x, p.v[1] = v.y;
       }
-      p.ks = blk[B::k_scale_lane(lane)];
-      p.vs = *reinterpret_cast<const uint32_t*>(blk + B::kVScale + 4 * qd);
+      p.ks = blk[oks];
+      p.vs = *reinterpret_cast<const uint32_t*>(blk + ovs);
       return p;
     };
     // Keys of the page pair j, j + 1 (a last single page stands in for its second).
