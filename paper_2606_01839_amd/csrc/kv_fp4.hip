@@ -427,9 +427,10 @@ __global__ __launch_bounds__(256) void kv_unpack_fp4_kernel(LaunchMeta, const ui
 }
 
 // ---------------------------------------------------------------------------------------------
-// Pack of a bf16 pool's conversation in 4 bits: one wave per (logical page, layer, kv head). A lane loads
-// from the bf16 block just the values whose codes it holds in the 4-bit one, so nothing is transposed: the
-// scale of a K group needs its lane only (D = 64: two), that of a V token the 16 lanes of a row.
+// Pack of a bf16 pool's conversation in 4 bits: one wave per (logical page, layer, kv head). Nothing is
+// transposed: the bf16 block too has K in groups of 32 dims, token by token (lane = 4 token + a quarter of the
+// group, a word of codes each), and V by dims (a lane loads the four tokens' values whose codes it holds). The scale
+// of a K group needs 4 lanes, that of a V token the 16 lanes of a row.
 // ---------------------------------------------------------------------------------------------
 template <int D>
 __global__ __launch_bounds__(256) void kv_pack_fp4_kernel(const uint16_t* __restrict__ pool, int64_t n_pages, int n_kv_heads,
@@ -448,24 +449,22 @@ __global__ __launch_bounds__(256) void kv_pack_fp4_kernel(const uint16_t* __rest
   uint4 kx[NW];
   uint2 vx[2 * NW];
 #pragma unroll
-  for (int i = 0; i < NW; ++i) kx[i] = ld16_nt(src + k_elem(c, NW * qd + i));
+  for (int i = 0; i < NW; ++i) kx[i] = ld16_nt(src + 512 * i + 8 * lane);
 #pragma unroll
   for (int t = 0; t < 2 * NW; ++t) vx[t] = ld8_nt(src + kPageTokens * D + (16 * t + c) * kPageTokens + 4 * qd);
 
-  // K: key c, dims (D / 4) qd ..
-  float f[NW][8];
-  uint32_t m = 0;
+  // K: token lane / 4, dims 32 i + 8 (lane % 4) ..
+  const bool k_in = lane / 4 < valid;
+  uint32_t kb = 0, kw[NW];
 #pragma unroll
   for (int i = 0; i < NW; ++i) {
-    if (c >= valid) kx[i] = make_uint4(0, 0, 0, 0);
-    unpack8(kx[i], f[i]);
-    m = dpp_max(m, max_bits(f[i]));
+    float f[8];
+    if (!k_in) kx[i] = make_uint4(0, 0, 0, 0);
+    unpack8(kx[i], f);
+    const uint32_t b = fp4_scale_byte(group_max<4>(max_bits(f)));
+    kw[i] = fp4_encode8(f, fp4_scale(b));
+    kb |= (k_in ? b : 0u) << (8 * i);
   }
-  if constexpr (D == 64) m = dpp_max(m, __float_as_uint(xor_shfl(__uint_as_float(m), 16)));
-  const uint32_t kb = fp4_scale_byte(m);
-  uint32_t kw[NW];
-#pragma unroll
-  for (int i = 0; i < NW; ++i) kw[i] = fp4_encode8(f[i], fp4_scale(kb));
   // V: keys 4 qd .. 4 qd + 3 of dims 16 t + c
   uint32_t vm[4] = {0, 0, 0, 0};
 #pragma unroll
@@ -493,14 +492,14 @@ __global__ __launch_bounds__(256) void kv_pack_fp4_kernel(const uint16_t* __rest
                         bf16_lo(b.x) * inv[0], bf16_hi(b.x) * inv[1], bf16_lo(b.y) * inv[2], bf16_hi(b.y) * inv[3]};
     vw[j] = fp4_encode8(x, 1.f);
   }
-  if constexpr (D == 128) {
-    st16(dst + B::k_lane(lane), make_uint4(kw[0], kw[1], kw[2], kw[3]));
-    st16(dst + B::kV + 16 * lane, make_uint4(vw[0], vw[1], vw[2], vw[3]));
-  } else {
-    st8(dst + B::k_lane(lane), make_uint2(kw[0], kw[1]));
-    st8(dst + B::kV + 8 * lane, make_uint2(vw[0], vw[1]));
+#pragma unroll
+  for (int i = 0; i < NW; ++i) *reinterpret_cast<uint32_t*>(dst + B::kK + 256 * i + 4 * lane) = kw[i];
+  if constexpr (D == 128) st16_nt(dst + B::kV + 16 * lane, make_uint4(vw[0], vw[1], vw[2], vw[3]));
+  else st8(dst + B::kV + 8 * lane, make_uint2(vw[0], vw[1]));
+  if ((lane & 3) == 0) {
+    if constexpr (D == 128) *reinterpret_cast<uint32_t*>(dst + B::kKScale + lane) = kb;
+    else *reinterpret_cast<uint16_t*>(dst + B::kKScale + lane / 2) = static_cast<uint16_t>(kb);
   }
-  if (D == 128 || (qd & 1) == 0) dst[B::k_scale_lane(lane)] = static_cast<uint8_t>(c < valid ? kb : 0);
   if (c == 0) *reinterpret_cast<uint32_t*>(dst + B::kVScale + 4 * qd) = vb;
   if (lane < (B::kBytes - B::kPad) / 16) st16(dst + B::kPad + 16 * lane, make_uint4(0, 0, 0, 0));
 }
