@@ -101,9 +101,10 @@ __device__ __forceinline__ uint32_t fp4_key_bits(int qd, int lo, int hi) {
 // The score product. K's codes and scales are operands of the MX matrix instructions as they lie in the page,
 // at four times the rate of bf16 if the other operand has 6 bits or fewer (measured: a 32x32x64 product of
 // 4 by 6 bits takes the 39 cycles of a 32x32x16 one in bf16, of 4 by 8 bits 73). So a query enters as the sum of three
-// e3m2 numbers, of 3 significant bits each and scales 2^0, 2^-3, 2^-6 of the first's: with the largest
-// magnitude of a block of 32 dims scaled to [8, 16) the sum is a bf16 query's 8 bits exactly for values down
-// to 2^-6 of the largest, and within 2^-14 of the largest for all. Three products cost 3/4 of the bf16 one
+// e3m2 numbers, of 3 significant bits each and scales 2^0, 2^-4, 2^-8 of the first's: with the largest
+// magnitude of a block of 32 dims scaled to [8, 16) each takes what the one before left (at most 1 of the
+// first's units, 16 of its own; the format ends at 28), and the sum is a bf16 query's 8 bits exactly for values
+// down to 2^-8 of the largest, and within 2^-16 of the largest for all. Three products cost 3/4 of the bf16 one
 // and no conversion of K. (Two e4m3 numbers are exact over a wider range but cost as much as bf16; two of
 // e2m3 are within 2^-10 of the largest only: as much as the softmax weights' rounding.)
 // ------------------------------------------------------------------------------------------------
@@ -144,12 +145,13 @@ __device__ __forceinline__ Bf6Query split_query(const uint4 (&x)[4]) {
       m = max(m, max(abs_bits(bf16_lo(w[j])), abs_bits(bf16_hi(w[j]))));
     }
   }
-  const uint32_t top = max(m >> 23, 10u);   // at least 2^-117: smaller queries lose bits of scores below 2^-100
+  const uint32_t top = max(m >> 23, 12u);   // at least 2^-115: smaller queries lose bits of scores below 2^-100
   Bf6Query q;
-  q.scale = (top - 3) | (top - 6) << 8 | (top - 9) << 16;
+  // (e3m2 has no infinity or NaN: a block with one gets the scale that makes its scores NaN)
+  q.scale = top == 255 ? 0xFFFFFFu : (top - 3) | (top - 7) << 8 | (top - 11) << 16;
 #pragma unroll
   for (int k = 0; k < 3; ++k) {
-    const float s = fp4_scale(top - 3 - 3 * k);
+    const float s = fp4_scale(top - 3 - 4 * k);
     q.p[k] = to_bf6(even, odd, s);
     if (k == 2) break;
     const f32x32 back = from_bf6(q.p[k], s);

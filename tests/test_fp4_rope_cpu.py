@@ -58,6 +58,27 @@ def test_rotate_by_hand():
     assert np.allclose(orope.rotate(x, [0], f), x)
 
 
+def test_a_query_is_the_sum_of_three_e3m2_numbers():
+    """The arithmetic of the score product over 4-bit pages: with the largest magnitude of a block scaled to
+    [8, 16), rounding to e3m2 (values to 28, 3 significant bits, subnormal step 1/16) three times, each time
+    what is left times 16, gives a bf16 value exactly down to 2^-8 of the largest and within 2^-16 of it."""
+    grid = np.array(sorted({m / 16 for m in range(4)} | {(4 + m) / 4 * 2.0 ** e for m in range(4) for e in range(-2, 5)}))
+
+    def e3m2(x):
+        d = np.abs(np.abs(x)[:, None] - grid)
+        near = np.where(d == d.min(1, keepdims=True), np.arange(32) + 32 * (np.arange(32) % 2), 99).min(1) % 32
+        return np.sign(x) * grid[near]
+
+    x = np.array([(128 + m) * 2.0 ** e for m in range(128) for e in range(-30, -3)])   # every bf16 value below 16
+    left, total = x.copy(), np.zeros_like(x)
+    for k in range(3):
+        part = e3m2(left * 16.0 ** k)
+        assert np.abs(left * 16.0 ** k).max() <= 16
+        total += part / 16.0 ** k
+        left = x - total
+    assert (left[x >= 8 * 2.0 ** -8] == 0).all() and np.abs(left).max() <= 8 * 2.0 ** -16
+
+
 # ---- host side of the library ----------------------------------------------------------------------
 @pytest.mark.parametrize("r", [16, 48, 64, 128])
 @pytest.mark.parametrize("scaling", ["none", "linear", "ntk", "parts"])

@@ -6,8 +6,8 @@ import pytest
 import torch
 
 from oracle import fp4 as o4
-from oracle.attention import attend_last
-from tests.helpers import assert_close, assert_within_arith_bound, f64, kv_tokens, q_tokens
+from oracle.attention import attend_last, attend_rows, weights
+from tests.helpers import arith_bound, assert_close, assert_within_arith_bound, f64, half_ulp_bf16, kv_tokens, q_tokens
 
 pytestmark = pytest.mark.gpu
 
@@ -264,7 +264,6 @@ def test_long_prefill_and_many_tiles(hq, hkv, d):
     row = 0
     for i, m in enumerate(lens):
         rows = np.unique(np.r_[0:70, m // 2:m // 2 + 40, m - 70:m])
-        from oracle.attention import attend_rows
         hk, hv = (x[0] for x in _held(*kv[i]))
         assert_close(out[row + torch.from_numpy(rows)], attend_rows(f64(q[i][rows]), rows, hk, hv), f"prefill {m}")
         row += m
@@ -297,6 +296,65 @@ def test_hard_attention_within_the_arithmetic_bound(d, profile):
     ref = attend_last(f64(q), hk, hv)
     assert_within_arith_bound(ext, f64(q), np.arange(L - n, L), hk, hv, ref, f"extend {profile}")
     assert_within_arith_bound(dec, f64(q[-1:]), [L - 1], hk, hv, ref[-1:], f"decode {profile}")
+    pool.close()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_queries_with_outliers(d):
+    """One dim of a query far larger than the other 31 of its block, which the score product then holds to
+    2^-16 of it (down to 2^-8 of it exactly): the arithmetic bound, and what that does to the weights."""
+    hq, hkv, L, n = 4, 2, 200, 8
+    r = np.random.default_rng(8)
+    k, v, q = r.standard_normal((L, hkv, d)), r.standard_normal((L, hkv, d)), r.standard_normal((n, hq, d))
+    k[:, :, 3] *= 2.0 ** -9
+    q[:, :, 3] = 700.0 * np.sign(q[:, :, 3])
+    k, v, q = (torch.from_numpy(x).to(torch.bfloat16) for x in (k, v, q))
+    pool = _pool(1, hq, hkv, d, 32)
+    c = pool.conv_create()
+    pool.kv_append(c, k[None].cuda(), v[None].cuda())
+    hk, hv = o4.held(f64(k), f64(v))
+    ext = pool.attn_extend([c], [n], 0, q.cuda())
+    dec = pool.attn_decode_batch([c], 0, q[-1:].contiguous().cuda())
+    torch.cuda.synchronize()
+    qf = f64(q)
+    ref = attend_last(qf, hk, hv)
+    pos = np.arange(L - n, L)
+    tol = arith_bound(qf, pos, hk, hv, ref) + half_ulp_bf16(ref)
+    for h in range(hq):
+        g = h // (hq // hkv)
+        top = np.abs(qf[:, h].reshape(n, d // 32, 32)).max(-1)
+        moved = 2.0 ** -16 / np.sqrt(d) * np.einsum("rb,jb->rj", top, np.abs(hk[:, g].reshape(L, d // 32, 32)).sum(-1)).max(-1)
+        w = weights(qf[:, h], pos, hk[:, g])
+        mad = np.einsum("rj,rjd->rd", w, np.abs(hv[None, :w.shape[1], g] - ref[:, h][:, None]))
+        tol[:, h] += np.expm1(2 * moved)[:, None] * mad
+    assert (np.abs(f64(ext) - ref) <= tol).all()
+    assert (np.abs(f64(dec) - ref[-1:]) <= tol[-1:]).all()
+    pool.close()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_query_that_is_not_finite_spoils_its_own_rows_only(d):
+    hq, hkv, lens, new = 8, 2, [70, 300, 33], [5, 40, 1]
+    pool = _pool(1, hq, hkv, d, 64)
+    convs, kv = _fill(pool, 1, lens, hkv, d)
+    q = [q_tokens(SEED, i, 0, n - m, m, hq, d) for i, (n, m) in enumerate(zip(lens, new))]
+    ref = np.concatenate([attend_last(f64(x), *[y[0] for y in _held(*kv[i])]) for i, x in enumerate(q)])
+    q = torch.cat(q)
+    q[2, 3, 40], q[20, 7, 0] = float("nan"), float("inf")
+    ext = pool.attn_extend(convs, new, 0, q.cuda())
+    last = [4, 44, 45]     # the conversations' last rows
+    qd = q[last].clone()
+    qd[1, 4, 10] = float("-inf")
+    dec = pool.attn_decode_batch(convs, 0, qd.contiguous().cuda())
+    torch.cuda.synchronize()
+    # (The other rows of a wave keep their tolerance, not their bits: a row that is not finite has the wave refresh its
+    # running maxima in every tile, so their weights are rounded against other maxima.)
+    for got, want, where in ((ext, ref, [(2, 3), (20, 7)]), (dec, ref[last], [(1, 4)])):
+        spoilt = np.zeros(want.shape[:2], dtype=bool)
+        for i in where:
+            spoilt[i] = True
+        assert np.isnan(f64(got.cpu())[spoilt]).all()
+        assert_close(got.cpu()[torch.from_numpy(~spoilt)], want[~spoilt])
     pool.close()
 
 
@@ -363,6 +421,31 @@ def test_mixed_step_equals_separate_calls(hq, hkv, d, ordered):
         for r, i in enumerate(dec):
             hk, hv = (x[l] for x in _held(*kv[i]))
             assert_close(od[l, r:r + 1], attend_last(f64(q[i][l]), hk, hv), f"layer {l} conv {i}")
+    pool.close()
+
+
+@pytest.mark.parametrize("hq,hkv,d,nl,P,n,dec,ordered", [
+    (32, 8, 128, 2, 1200, 300, [30000] * 12, True), (16, 8, 128, 2, 1200, 300, [30000] * 12, True),
+    (32, 8, 64, 2, 1200, 300, [30000] * 12, True), (32, 8, 128, 24, 1500, 500, [2100, 700], False),
+    (32, 8, 64, 24, 1200, 300, [2100, 700], False), (32, 8, 64, 24, 1500, 500, [2100, 700], False)])
+def test_chained_tiles(hq, hkv, d, nl, P, n, dec, ordered):
+    """Sizes at which a mixed step has one workgroup take a cut tile's pieces in turn, as in a layer's launch beside
+    a large decode or in one launch of all layers: the same bits as the separate calls, which give each piece a workgroup."""
+    lens, new, m = [P] + dec, [n] + [1] * len(dec), len(dec)
+    pool = _pool(nl, hq, hkv, d, sum((a + b + 15) // 16 for a, b in zip(lens, new)) + 16, max_pages=2048, max_convs=16)
+    g = torch.Generator(device="cuda").manual_seed(7)
+    rand = lambda *s: torch.randn(s, generator=g, device="cuda").to(torch.bfloat16)
+    convs = [pool.conv_create() for _ in lens]
+    pool.kv_append_batch(convs, lens, rand(nl, sum(lens), hkv, d), rand(nl, sum(lens), hkv, d))
+    qe, qd = rand(nl, n, hq, d), rand(nl, m, hq, d)
+    oe, od = pool.mixed_step(convs[:1], [n], convs[1:], rand(nl, n + m, hkv, d), rand(nl, n + m, hkv, d), qe, qd, layer_ordered=ordered)
+    for l in range(nl):
+        assert torch.equal(pool.attn_extend(convs[:1], [n], l, qe[l]), oe[l]), l
+        assert torch.equal(pool.attn_decode_batch(convs[1:], l, qd[l]), od[l]), l
+    k, v = pool.kv_read(convs[:1], [0], [P + n])
+    torch.cuda.synchronize()
+    rows = [0, n // 2, n - 1]
+    assert_close(oe[-1, rows].cpu(), attend_rows(f64(qe[-1, rows].cpu()), [P + r for r in rows], f64(k[-1].cpu()), f64(v[-1].cpu())))
     pool.close()
 
 
