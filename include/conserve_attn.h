@@ -319,6 +319,17 @@ cs_status cs_mixed_step(cs_pool* pool, int32_t n_ext, const cs_conv* ext_convs,
                         const void* q_dec, void* out_dec, uint32_t flags, cs_stream stream);
 
 /*
+ * The same step of a model with rotary positions: the new tokens' keys enter the cache turned by their positions (as
+ * cs_kv_append_rope) and every query attends turned by its own (as cs_rope_q). q_ext and q_dec are left as they are,
+ * unless the outputs are the same tensors (out_ext == q_ext, out_dec == q_dec), which is allowed; otherwise
+ * inputs and outputs do not overlap. Errors: as cs_mixed_step, and as cs_kv_append_rope for rope.
+ */
+cs_status cs_mixed_step_rope(cs_pool* pool, const cs_rope* rope, int32_t n_ext, const cs_conv* ext_convs,
+                             const int32_t* ext_lens, int32_t n_dec, const cs_conv* dec_convs, const void* k, const void* v,
+                             const void* q_ext, void* out_ext, const void* q_dec, void* out_dec, uint32_t flags,
+                             cs_stream stream);
+
+/*
  * Version of the transfer wire format of cs_kv_pack / cs_kv_unpack below. The format is frozen at
  * this version: it is the pool's block format as of version 1, and a later change of the pool's
  * private block layout keeps pack and unpack reading and writing exactly this format (a new format

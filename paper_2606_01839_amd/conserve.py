@@ -33,7 +33,7 @@ EXPORTS = [
     "cs_pool_occupancy", "cs_conv_create", "cs_conv_destroy", "cs_conv_len", "cs_conv_pages",
     "cs_kv_append", "cs_kv_append_batch", "cs_attn_prefill_turn1", "cs_attn_extend",
     "cs_attn_decode_batch", "cs_attn_decode_batch_noalloc", "cs_mixed_step", "cs_kv_pack_size", "cs_kv_pack", "cs_kv_unpack",
-    "cs_pool_kv_bytes_as", "cs_pool_create_as", "cs_rope_init", "cs_kv_append_rope", "cs_rope_q", "cs_kv_read",
+    "cs_pool_kv_bytes_as", "cs_pool_create_as", "cs_rope_init", "cs_kv_append_rope", "cs_rope_q", "cs_kv_read", "cs_mixed_step_rope",
     "cs_kv_pack_fp4_size", "cs_kv_pack_fp4",
     "cs_profile_start",
     "cs_profile_stop", "cs_device_info", "cs_probe_stream_read", "cs_debug_fail_launches",
@@ -101,6 +101,8 @@ def load_library(path: str = _LIB_PATH) -> ctypes.CDLL:
         "cs_rope_init": (I32, [ctypes.POINTER(RopeDesc), I32, I32, ctypes.c_double, I32] + [ctypes.c_double] * 4),
         "cs_kv_append_rope": (I32, [P, ctypes.POINTER(RopeDesc), I32, VP, VP, VP, VP, VP, VP, VP]),
         "cs_rope_q": (I32, [P, ctypes.POINTER(RopeDesc), I32, VP, VP, I32, VP, VP, VP]),
+        "cs_mixed_step_rope": (I32, [P, ctypes.POINTER(RopeDesc), I32, VP, VP, I32, VP, VP, VP, VP, VP, VP, VP,
+                                     ctypes.c_uint32, VP]),
         "cs_kv_read": (I32, [P, I32, VP, VP, VP, VP, VP, VP]),
         "cs_kv_pack_fp4_size": (I32, [P, I32, ctypes.POINTER(SZ)]),
         "cs_kv_pack_fp4": (I32, [P, I32, VP, SZ, VP]),
@@ -462,11 +464,12 @@ class KVPool:
         return out
 
     def mixed_step(self, ext_convs, ext_lens, dec_convs, k, v, q_ext=None, q_dec=None,
-                   out_ext=None, out_dec=None, layer_ordered=False):
+                   out_ext=None, out_dec=None, layer_ordered=False, rope: Rope | None = None):
         """One decoder step: extend chunks + one decoded token per decoding conversation, appended
         for every layer, then attention of every layer. With layer_ordered, layer l+1's attention
         starts only after layer l's (extend and decode of one layer still overlap), as in a model
-        forward pass. Returns (out_ext, out_dec)."""
+        forward pass. With rope the new tokens' keys and queries turn by their positions
+        (cs_mixed_step_rope). Returns (out_ext, out_dec)."""
         ea, ep = _i32_array(ext_convs)
         la, lp = _i32_array(ext_lens)
         da, dp = _i32_array(dec_convs)
@@ -482,15 +485,18 @@ class KVPool:
             qe = self._dev(q_ext, "q_ext", eshape)
             if out_ext is None:
                 out_ext = torch.empty(eshape, dtype=torch.bfloat16, device=self.device)
-            oe = self._dev(out_ext, "out_ext", eshape)
+            oe = self._dev(out_ext, "out_ext", eshape) if rope is None else self._rotated(q_ext, out_ext, "out_ext", eshape)
         if nd:
             qd = self._dev(q_dec, "q_dec", dshape)
             if out_dec is None:
                 out_dec = torch.empty(dshape, dtype=torch.bfloat16, device=self.device)
-            od = self._dev(out_dec, "out_dec", dshape)
+            od = self._dev(out_dec, "out_dec", dshape) if rope is None else self._rotated(q_dec, out_dec, "out_dec", dshape)
         flags = CS_MIXED_LAYER_ORDERED if layer_ordered else 0
-        _check(self.lib.cs_mixed_step(self._handle, len(ea), ep, lp, nd, dp, kp, vp, qe, oe, qd, od,
-                                      flags, _stream_handle(self.device)))
+        args = (len(ea), ep, lp, nd, dp, kp, vp, qe, oe, qd, od, flags, _stream_handle(self.device))
+        if rope is None:
+            _check(self.lib.cs_mixed_step(self._handle, *args))
+        else:
+            _check(self.lib.cs_mixed_step_rope(self._handle, ctypes.byref(rope.desc), *args))
         return out_ext, out_dec
 
     # -- instrumentation -----------------------------------------------------------------------

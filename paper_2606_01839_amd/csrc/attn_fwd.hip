@@ -317,7 +317,12 @@ __device__ __forceinline__ void attn_fwd_block(const ExtendArgs& a, const int bl
   Bf6Query query[KM];
   if constexpr (FP4) {
 #pragma unroll
-    for (int ks = 0; ks < KM; ++ks) query[ks] = split_query(q4[ks]);   // padding rows: row 0's (not stored)
+    for (int ks = 0; ks < KM; ++ks) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (!valid) q4[ks][i] = make_uint4(0, 0, 0, 0);
+      query[ks] = split_query(q4[ks]);
+    }
   } else {
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {

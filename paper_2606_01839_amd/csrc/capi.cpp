@@ -1169,11 +1169,17 @@ cs_status cs_kv_unpack(cs_pool* p, const void* src, size_t src_bytes, int64_t n_
   return CS_OK;
 }
 
-cs_status cs_mixed_step(cs_pool* p, int32_t n_ext, const cs_conv* ext_convs, const int32_t* ext_lens,
-                        int32_t n_dec, const cs_conv* dec_convs, const void* k, const void* v,
-                        const void* q_ext, void* out_ext, const void* q_dec, void* out_dec,
-                        uint32_t flags, cs_stream stream) {
+// `rope` (may be null): the new tokens' keys and queries turn by their positions.
+static cs_status mixed_impl(cs_pool* p, const cs_rope* rope, int32_t n_ext, const cs_conv* ext_convs, const int32_t* ext_lens,
+                            int32_t n_dec, const cs_conv* dec_convs, const void* k, const void* v,
+                            const void* q_ext, void* out_ext, const void* q_dec, void* out_dec,
+                            uint32_t flags, cs_stream stream) {
   if (!p) return fail(CS_EINVAL, "null pool");
+  RotatedAppend rotated;
+  if (rope) {
+    const cs_status rs = rope_args(p->desc, rope, &rotated.rope);
+    if (rs != CS_OK) return rs;
+  }
   if (n_ext < 0 || n_dec < 0) return fail(CS_EINVAL, "negative batch size");
   if (flags & ~static_cast<uint32_t>(CS_MIXED_LAYER_ORDERED)) return fail(CS_EINVAL, "unknown flags");
   if ((n_ext > 0 && (!ext_convs || !ext_lens)) || (n_dec > 0 && !dec_convs))
@@ -1241,10 +1247,31 @@ cs_status cs_mixed_step(cs_pool* p, int32_t n_ext, const cs_conv* ext_convs, con
                                               e_plan.tiles.size() * sizeof(cs::ExtendTile) +
                                               e_plan.merges.size() * sizeof(cs::ExtendMerge) + 64 <= kQuarter;
   if (e_carried) ew.parts.push_back(push_extend(e_plan, 0, e_plan.tiles.size(), &blob, &e_off));
+  if (rope) {
+    // Queries first, into the output tensors, where the attention reads them: a workgroup (or its merge) writes
+    // rows that only it, or launches before it, read. In front of the append, so that their metadata is not
+    // in the ring behind plans that wait for their launches.
+    std::vector<cs::RopeConv> re, rd;
+    int32_t row = 0;
+    for (int32_t i = 0; i < n_ext; ++i) {
+      re.push_back({row, static_cast<int32_t>(cv[i]->len)});
+      row += ext_lens[i];
+    }
+    for (int32_t i = 0; i < n_dec; ++i) rd.push_back({i, static_cast<int32_t>(cv[n_ext + i]->len)});
+    if (std::max(re.size(), rd.size()) * sizeof(cs::RopeConv) > kQuarter)
+      return fail(CS_ENOMEM, "batch descriptor exceeds the metadata ring");
+    if ((st = ensure_device(p)) != CS_OK) return st;
+    if ((st = use_stream(p, as_stream(stream))) != CS_OK) return st;
+    if (n_ext > 0) st = run_rope_q(p, re, ext_rows, p->desc.n_layers, rotated.rope, q_ext, out_ext);
+    if (n_dec > 0 && st == CS_OK) st = run_rope_q(p, rd, n_dec, p->desc.n_layers, rotated.rope, q_dec, out_dec);
+    if (st != CS_OK) return st;
+    q_ext = out_ext;
+    q_dec = out_dec;
+  }
   // append every new token (all layers); validates capacity and commits the host metadata
   void* dev = nullptr;
-  if ((st = append_impl(p, static_cast<int32_t>(all.size()), all.data(), n_new.data(), k, v, stream, &blob, &dev)) !=
-      CS_OK)
+  if ((st = append_impl(p, static_cast<int32_t>(all.size()), all.data(), n_new.data(), k, v, stream, &blob, &dev,
+                        rope ? &rotated : nullptr)) != CS_OK)
     return st;
   if (n_dec > 0) dw.w.meta = meta_part(dev, d_off, d_bytes);
   if (e_carried) ew.parts[0].meta = meta_part(dev, e_off, blob.bytes.size() - e_off);
@@ -1343,6 +1370,20 @@ cs_status cs_mixed_step(cs_pool* p, int32_t n_ext, const cs_conv* ext_convs, con
     if (st == CS_OK) st = sj;
   }
   return st;
+}
+
+cs_status cs_mixed_step(cs_pool* p, int32_t n_ext, const cs_conv* ext_convs, const int32_t* ext_lens,
+                        int32_t n_dec, const cs_conv* dec_convs, const void* k, const void* v,
+                        const void* q_ext, void* out_ext, const void* q_dec, void* out_dec,
+                        uint32_t flags, cs_stream stream) {
+  return mixed_impl(p, nullptr, n_ext, ext_convs, ext_lens, n_dec, dec_convs, k, v, q_ext, out_ext, q_dec, out_dec, flags, stream);
+}
+
+cs_status cs_mixed_step_rope(cs_pool* p, const cs_rope* rope, int32_t n_ext, const cs_conv* ext_convs, const int32_t* ext_lens,
+                             int32_t n_dec, const cs_conv* dec_convs, const void* k, const void* v, const void* q_ext,
+                             void* out_ext, const void* q_dec, void* out_dec, uint32_t flags, cs_stream stream) {
+  if (!rope) return fail(CS_EINVAL, "null rope");
+  return mixed_impl(p, rope, n_ext, ext_convs, ext_lens, n_dec, dec_convs, k, v, q_ext, out_ext, q_dec, out_dec, flags, stream);
 }
 
 cs_status cs_device_info(int32_t device, cs_device_info_t* out) {

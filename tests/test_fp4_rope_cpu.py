@@ -220,6 +220,14 @@ def test_refusals_change_nothing():
         assert lib.cs_rope_q(None, P, 1, cp, npp, 1, x, x, None) == CS_EINVAL
         assert lib.cs_kv_read(None, 1, cp, x, npp, x, x, None) == CS_EINVAL
         assert lib.cs_kv_read(p._handle, 1, cp, None, npp, x, x, None) == CS_EINVAL
+        refused(CS_EINVAL, p.mixed_step, [a], [1], [], z(1), z(1), z(1, 4), rope=wide)
+        refused(CS_EINVAL, p.mixed_step, [a], [1], [a], z(2), z(2), z(1, 4), z(1, 4), rope=rope)
+        refused(CS_ERANGE, p.mixed_step, [a], [129], [], z(129), z(129), z(129, 4), rope=rope)
+        assert lib.cs_mixed_step_rope(p._handle, None, 1, cp, npp, 0, None, x, x, x, x, None, None, 0, None) == CS_EINVAL
+        assert lib.cs_mixed_step_rope(p._handle, P, 1, cp, npp, 0, None, x, x, x, x, None, None, 2, None) == CS_EINVAL
+        assert lib.cs_mixed_step_rope(None, P, 1, cp, npp, 0, None, x, x, x, x, None, None, 0, None) == CS_EINVAL
+        with pytest.raises(ValueError, match="overlaps"):
+            p.mixed_step([a], [2], [], z(2), z(2), q, out_ext=shifted, rope=rope)
         n = ctypes.c_size_t()
         assert lib.cs_kv_pack_fp4_size(p._handle, 99, ctypes.byref(n)) == CS_ENOENT
         assert lib.cs_kv_pack_fp4_size(None, a, ctypes.byref(n)) == CS_EINVAL

@@ -259,6 +259,58 @@ def test_a_served_conversation(fmt, hq, hkv, d, r):
     dec.close()
 
 
+@pytest.mark.parametrize("fmt", ["bf16", "fp4"])
+@pytest.mark.parametrize("hq,hkv,d,r,inter", [(32, 8, 128, 128, False), (4, 2, 64, 32, True), (8, 8, 128, 64, False)])
+@pytest.mark.parametrize("ordered", [False, True])
+def test_mixed_step(fmt, hq, hkv, d, r, inter, ordered):
+    """A step with rotated keys and queries, its outputs apart from its queries or in their place: the same bits as
+    an append of rotated keys and queries and the separate calls on a second pool."""
+    nl = 2
+    rope = _rope(r, inter, "none")
+    lens, new = [300, 1, 1500, 64, 900, 9], [40, 1, 1, 130, 1, 17]
+    ext, dec = [0, 3, 5], [1, 2, 4]
+    kv = [kv_tokens(SEED, i, nl, 0, n + m, hkv, d) for i, (n, m) in enumerate(zip(lens, new))]
+    cat = lambda idx, j, new_part: torch.cat([kv[i][j][:, lens[i]:] if new_part else kv[i][j][:, :lens[i]] for i in idx], 1).contiguous().cuda()
+    q = [torch.stack([q_tokens(SEED, i, l, lens[i], new[i], hq, d) for l in range(nl)]) for i in range(6)]
+    qe, qd = (torch.cat([q[i] for i in g], 1).contiguous().cuda() for g in (ext, dec))
+    outs = []
+    for mode in range(3):
+        pool = _pool(nl, hq, hkv, d, 400, fmt)
+        convs = [pool.conv_create() for _ in lens]
+        pool.kv_append_rope(convs, lens, cat(range(6), 0, False), cat(range(6), 1, False), rope)
+        k, v = cat(ext + dec, 0, True), cat(ext + dec, 1, True)
+        e, x = [convs[i] for i in ext], [convs[i] for i in dec]
+        if mode < 2:
+            a, b = qe.clone(), qd.clone()
+            oe, od = pool.mixed_step(e, [new[i] for i in ext], x, k, v, a, b, layer_ordered=ordered, rope=rope,
+                                     **(dict(out_ext=a, out_dec=b) if mode else {}))
+            torch.cuda.synchronize()
+            assert mode or (torch.equal(a, qe) and torch.equal(b, qd))
+        else:
+            qr = pool.kv_append_rope(e + x, [new[i] for i in ext + dec], k, v, rope, q=torch.cat([qe, qd], 1).contiguous())
+            ne = qe.shape[1]
+            oe = torch.stack([pool.attn_extend(e, [new[i] for i in ext], l, qr[l, :ne].contiguous()) for l in range(nl)])
+            od = torch.stack([pool.attn_decode_batch(x, l, qr[l, ne:].contiguous()) for l in range(nl)])
+        held = pool.kv_read(convs, [0] * 6, [n + m for n, m in zip(lens, new)])
+        torch.cuda.synchronize()
+        outs.append((oe, od) + held)
+        pool.close()
+    for other in outs[1:]:
+        assert all(torch.equal(x, y) for x, y in zip(outs[0], other))
+    # and against the oracle, on what the cache holds
+    k, v = (f64(x.cpu()) for x in outs[0][2:])
+    starts = np.cumsum([0] + [n + m for n, m in zip(lens, new)])
+    row = 0
+    for i in ext:
+        turned = torch.from_numpy(_turn(q[i], np.arange(lens[i], lens[i] + new[i]), rope)).to(torch.bfloat16)
+        part = slice(starts[i], starts[i + 1])
+        got = outs[0][0][1, row:row + new[i]]
+        ref = attend_last(f64(turned[1]), k[1, part], v[1, part])
+        # (a query may differ from the oracle's by a bf16 step of single dims: twice the attention's tolerance)
+        assert np.sqrt(((f64(got.cpu()) - ref) ** 2).sum() / (ref ** 2).sum()) <= 6e-3
+        row += new[i]
+
+
 def test_scores_depend_on_distance_only():
     """What rotary positions are for: the same query and keys at another place give the same weights."""
     from paper_2606_01839_amd import Rope
