@@ -170,39 +170,31 @@ __device__ __forceinline__ void split_body(const DecodeArgs& a, const int work, 
           vs[r] = in ? vs[r] : 0.f;
         }
       }
-      // Weights against the running maximum, which is refreshed only where a lane's sum exceeds 2^8 or is not
-      // finite (always in the first step), as in the attention kernel: no maximum and no exchange between
-      // lanes on the common path.
-      float p[8];
-      uint4 pw;
-      auto weights = [&] {
-        float ps0 = 0.f, ps1 = 0.f;
+      float mx = x[0];
 #pragma unroll
-        for (int r = 0; r < 8; ++r) p[r] = fast_exp2(__builtin_fmaf(x[r], a.scale_log2, -m_run));
-        pw = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
-        // The denominator sums the same bf16-rounded weights the PV product uses: scaling by the values' power
-        // of two commutes with the rounding.
-        ps0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pw.x), ones, ps0, false);
-        ps1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pw.y), ones, ps1, false);
-        ps0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pw.z), ones, ps0, false);
-        ps1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pw.w), ones, ps1, false);
-        return ps0 + ps1;
-      };
-      float ps = weights();
-      if (__builtin_amdgcn_ballot_w64(!(ps <= 256.f)) != 0) {
-        float mx = x[0];
-#pragma unroll
-        for (int r = 1; r < 8; ++r) mx = fmaxf(mx, x[r]);
-        mx = fmaxf(mx, xor_shfl(mx, 16));
-        mx = fmaxf(mx, xor_shfl(mx, 32));
-        const float m_new = fmaxf(m_run, mx * a.scale_log2);
+      for (int r = 1; r < 8; ++r) mx = fmaxf(mx, x[r]);
+      mx = fmaxf(mx, xor_shfl(mx, 16));
+      mx = fmaxf(mx, xor_shfl(mx, 32));
+      const float m_new = fmaxf(m_run, mx * a.scale_log2);
+      if (__builtin_amdgcn_ballot_w64(!(m_new <= m_run)) != 0) {
         const float alpha = fast_exp2(m_run - m_new);
         m_run = m_new;
         l_run *= alpha;
 #pragma unroll
         for (int t = 0; t < DT; ++t) o[t] *= alpha;
-        ps = weights();
       }
+      float p[8];
+#pragma unroll
+      for (int r = 0; r < 8; ++r) p[r] = fast_exp2(__builtin_fmaf(x[r], a.scale_log2, -m_run));
+      const uint4 pw = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
+      // The denominator sums the same bf16-rounded weights the PV product uses: scaling by the values' power
+      // of two commutes with the rounding.
+      float ps0 = 0.f, ps1 = 0.f;
+      ps0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pw.x), ones, ps0, false);
+      ps1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pw.y), ones, ps1, false);
+      ps0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pw.z), ones, ps0, false);
+      ps1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pw.w), ones, ps1, false);
+      const float ps = ps0 + ps1;
       l_run += ps;
       const bf16x8 pop = as_bf16x8(make_uint4(pack_bf16x2(p[0] * vs[0], p[1] * vs[1]), pack_bf16x2(p[2] * vs[2], p[3] * vs[3]),
                                               pack_bf16x2(p[4] * vs[4], p[5] * vs[5]), pack_bf16x2(p[6] * vs[6], p[7] * vs[7])));
