@@ -201,7 +201,8 @@ cs_status cs_rope_init(cs_rope* out, int32_t rotary_dim, int32_t interleaved, do
  * null) the queries of the same tokens, [n_layers][sum(n_new)][n_q_heads][head_dim], are rotated in the same
  * launch into q_out (same shape; q itself, or no overlap with it), ready for the attention calls.
  * Errors: as cs_kv_append_batch; CS_EINVAL for a null or invalid rope (rotary_dim no multiple of 16 in
- * 16 .. head_dim, interleaved not 0 or 1, amplitude or an inv_freq in use not finite), q without q_out.
+ * 16 .. head_dim, interleaved not 0 or 1, amplitude or an inv_freq in use not finite), q without q_out, q of more
+ * than 2^28 - 16 rows. After CS_EHIP q_out is undefined: queries rotated in place may or may not have turned.
  */
 cs_status cs_kv_append_rope(cs_pool* pool, const cs_rope* rope, int32_t n_convs, const cs_conv* convs, const int32_t* n_new,
                             const void* k, const void* v, const void* q, void* q_out, cs_stream stream);
@@ -209,7 +210,8 @@ cs_status cs_kv_append_rope(cs_pool* pool, const cs_rope* rope, int32_t n_convs,
 /*
  * Queries of the last q_lens[i] positions of each conversation (those the attention calls take), rotated:
  * q, out [n_layers][sum(q_lens)][n_q_heads][head_dim] for any n_layers >= 0; out may be q itself, otherwise
- * they do not overlap. Errors: as cs_attn_extend, and as cs_kv_append_rope for rope; CS_EINVAL (n_layers < 0).
+ * they do not overlap. Errors: as cs_attn_extend, and as cs_kv_append_rope for rope and after CS_EHIP; CS_EINVAL
+ * (n_layers < 0, more than 2^28 - 16 rows).
  */
 cs_status cs_rope_q(cs_pool* pool, const cs_rope* rope, int32_t n_convs, const cs_conv* convs, const int32_t* q_lens,
                     int32_t n_layers, const void* q, void* out, cs_stream stream);
@@ -322,7 +324,8 @@ cs_status cs_mixed_step(cs_pool* pool, int32_t n_ext, const cs_conv* ext_convs,
  * The same step of a model with rotary positions: the new tokens' keys enter the cache turned by their positions (as
  * cs_kv_append_rope) and every query attends turned by its own (as cs_rope_q). q_ext and q_dec are left as they are,
  * unless the outputs are the same tensors (out_ext == q_ext, out_dec == q_dec), which is allowed; otherwise
- * inputs and outputs do not overlap. Errors: as cs_mixed_step, and as cs_kv_append_rope for rope.
+ * inputs and outputs do not overlap. Errors: as cs_mixed_step, and as cs_kv_append_rope for rope and rows; a batch
+ * that the pool cannot take is refused before a query turns, but after CS_EHIP the outputs are undefined.
  */
 cs_status cs_mixed_step_rope(cs_pool* pool, const cs_rope* rope, int32_t n_ext, const cs_conv* ext_convs,
                              const int32_t* ext_lens, int32_t n_dec, const cs_conv* dec_convs, const void* k, const void* v,

@@ -653,9 +653,13 @@ struct RotatedAppend {
   void* q_out = nullptr;
 };
 
+// Rows a query rotation takes at most: 16 a workgroup of 256, and a grid has fewer than 2^32 threads.
+constexpr int64_t kMaxRopeRows = (int64_t(1) << 28) - 16;
+
 // Queries [n_layers][rows][n_q_heads][head_dim] rotated in launches of their own.
 cs_status run_rope_q(cs_pool* p, const std::vector<cs::RopeConv>& convs, int64_t rows, int32_t n_layers, const cs::RopeArgs& rope,
                      const void* q, void* out) {
+  if (rows > kMaxRopeRows) return fail(CS_EINVAL, "too many query rows");
   Blob b;
   b.push(convs.data(), convs.size());
   if (b.bytes.size() > kQuarter) return fail(CS_ENOMEM, "batch descriptor exceeds the metadata ring");
@@ -957,7 +961,7 @@ cs_status cs_rope_q(cs_pool* p, const cs_rope* rope, int32_t n, const cs_conv* c
     if (q_lens[i] < 0) return fail(CS_EINVAL, "negative q_len");
     if (q_lens[i] > cv[i]->len)
       return fail(CS_ESTATE, "q_len " + std::to_string(q_lens[i]) + " exceeds conversation length " + std::to_string(cv[i]->len));
-    if (rows + q_lens[i] > INT32_MAX) return fail(CS_EINVAL, "too many query rows");
+    if (rows + q_lens[i] > kMaxRopeRows) return fail(CS_EINVAL, "too many query rows");
     if (q_lens[i] > 0) rc.push_back({static_cast<int32_t>(rows), static_cast<int32_t>(cv[i]->len - q_lens[i])});
     rows += q_lens[i];
   }

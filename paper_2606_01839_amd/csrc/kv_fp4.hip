@@ -39,6 +39,8 @@ __device__ __forceinline__ PageChunk load_chunk(ConstPtr<PageChunk> p) {
 // A chunk that starts a page (t0 = 0) writes the whole block, zeros in slots [t1, 16); one that continues a
 // page writes only its slots. Two tokens of a 4-bit page share a byte of V: the wave that owns the (page,
 // head) puts its codes between the others'.
+// Bound by HBM: 12.5k tokens of 32 layers, 8 kv heads of 128 into 4-bit pages (2.09 GB read and written, by the
+// counters too) 350 us, 5.97 TB/s; 5.3k rotated into bf16 pages (1.39 GB) 236 us, 5.90 TB/s: the rotation costs nothing.
 // ---------------------------------------------------------------------------------------------
 struct AppendArgs {
   const void* meta;
@@ -304,7 +306,9 @@ __global__ __launch_bounds__(256) void rope_q_kernel(LaunchMeta, RopeArgs rope, 
 }
 
 // ---------------------------------------------------------------------------------------------
-// Read back: one wave per (chunk, layer, kv head); V through LDS into token rows.
+// Read back: one wave per (chunk, layer, kv head); V through LDS into token rows. Bound by HBM: 12.5k tokens of 32
+// layers, 8 kv heads of 128 out of 4-bit pages (2.09 GB read and written) 377 us, 5.54 TB/s; 5.3k out of bf16 pages (1.39 GB)
+// 243 us, 5.73 TB/s (283 with the K loads behind the V part and the cached forms).
 // ---------------------------------------------------------------------------------------------
 template <int D, bool FP4>
 __global__ __launch_bounds__(256) void kv_read_kernel(LaunchMeta, const void* meta, int n_kv_heads, const void* pool,
@@ -325,38 +329,58 @@ __global__ __launch_bounds__(256) void kv_read_kernel(LaunchMeta, const void* me
   };
   uint16_t* vt = reinterpret_cast<uint16_t*>(&vts[wave][0][0]);
   constexpr int kStride = D + 8;
+  // all loads before the first store (a chunk's pages are whole: slots outside [t0, t1) are read too)
+  uint4 kx[kPasses];
+  uint32_t kw[kPasses], kb[kPasses];
+#pragma unroll
+  for (int ps = 0; ps < kPasses; ++ps) {
+    const int t = t_lane + ps * kRows;
+    if constexpr (FP4) {
+      kw[ps] = *reinterpret_cast<const uint32_t*>(blk + B::k_word(t, ch));
+      kb[ps] = blk[B::k_scale(t, ch >> 2)];
+    } else {
+      kx[ps] = ld16_nt(blk16 + k_elem(t, ch));
+    }
+  }
   if constexpr (FP4) {
-    const uint32_t* src = reinterpret_cast<const uint32_t*>(blk + B::kV) + lane * B::kWords;
     const int col = lane & 15, qd = lane >> 4;
+    uint32_t w[B::kWords];
+    if constexpr (D == 128) {
+      const uint4 x = ld16(blk + B::kV + 16 * lane);
+      w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+    } else {
+      const uint2 x = ld8(blk + B::kV + 8 * lane);
+      w[0] = x.x, w[1] = x.y;
+    }
     const uint32_t vs = *reinterpret_cast<const uint32_t*>(blk + B::kVScale + 4 * qd);
+    __builtin_amdgcn_sched_barrier(0);
     const float s[4] = {fp4_scale_of(vs, 0), fp4_scale_of(vs, 1), fp4_scale_of(vs, 2), fp4_scale_of(vs, 3)};
 #pragma unroll
     for (int j = 0; j < B::kWords; ++j) {
-      const uint32_t w = src[j];
-      const uint2 lo = fp4_quad<0>(w, s), hi = fp4_quad<1>(w, s);
+      const uint2 lo = fp4_quad<0>(w[j], s), hi = fp4_quad<1>(w[j], s);
       const uint32_t x[4] = {lo.x, lo.y, hi.x, hi.y};
 #pragma unroll
       for (int e = 0; e < 8; ++e)   // tile 2 j + e / 4, key 4 qd + e % 4
         vt[(4 * qd + e % 4) * kStride + 16 * (2 * j + e / 4) + col] = static_cast<uint16_t>(x[e / 2] >> (16 * (e % 2)));
     }
   } else {
+    uint4 r[D / 64][2];
 #pragma unroll
-    for (int e = lane; e < D; e += 64) {
-      const uint4 r0 = ld16(blk16 + kPageTokens * D + e * kPageTokens), r1 = ld16(blk16 + kPageTokens * D + e * kPageTokens + 8);
-      const uint32_t x[8] = {r0.x, r0.y, r0.z, r0.w, r1.x, r1.y, r1.z, r1.w};
+    for (int i = 0; i < D / 64; ++i)
 #pragma unroll
-      for (int t = 0; t < kPageTokens; ++t) vt[t * kStride + e] = static_cast<uint16_t>(x[t / 2] >> (16 * (t % 2)));
+      for (int h = 0; h < 2; ++h) r[i][h] = ld16_nt(blk16 + kPageTokens * D + (lane + 64 * i) * kPageTokens + 8 * h);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) {
+      const uint32_t x[8] = {r[i][0].x, r[i][0].y, r[i][0].z, r[i][0].w, r[i][1].x, r[i][1].y, r[i][1].z, r[i][1].w};
+#pragma unroll
+      for (int t = 0; t < kPageTokens; ++t) vt[t * kStride + lane + 64 * i] = static_cast<uint16_t>(x[t / 2] >> (16 * (t % 2)));
     }
   }
 #pragma unroll
   for (int ps = 0; ps < kPasses; ++ps) {
     const int t = t_lane + ps * kRows;
-    if (t < c.t0 || t >= c.t1) continue;
-    if constexpr (FP4)
-      st16_nt(k + at(t), fp4_word(*reinterpret_cast<const uint32_t*>(blk + B::k_word(t, ch)),
-                               fp4_scale(blk[B::k_scale(t, ch >> 2)])));
-    else
-      st16_nt(k + at(t), ld16(blk16 + k_elem(t, ch)));
+    if (t >= c.t0 && t < c.t1) st16_nt(k + at(t), FP4 ? fp4_word(kw[ps], fp4_scale(kb[ps])) : kx[ps]);
   }
   __syncthreads();
 #pragma unroll
@@ -368,7 +392,8 @@ __global__ __launch_bounds__(256) void kv_read_kernel(LaunchMeta, const void* me
 
 // ---------------------------------------------------------------------------------------------
 // Pack and unpack of 4-bit pages: the blocks of a page's heads lie one after the other in the pool and in
-// the wire alike, so a workgroup copies one (layer, page) of all heads.
+// the wire alike, so a workgroup copies one (layer, page) of all heads. Bound by HBM: 3.8k tokens of 32 layers
+// unpacked (264 MB read and written) 49 us, 5.41 TB/s.
 // ---------------------------------------------------------------------------------------------
 // Word w of a block with the token slots >= valid zeroed.
 template <int D>
@@ -430,7 +455,8 @@ __global__ __launch_bounds__(256) void kv_unpack_fp4_kernel(LaunchMeta, const ui
 // Pack of a bf16 pool's conversation in 4 bits: one wave per (logical page, layer, kv head). Nothing is
 // transposed: the bf16 block too has K in groups of 32 dims, token by token (lane = 4 token + a quarter of the
 // group, a word of codes each), and V by dims (a lane loads the four tokens' values whose codes it holds). The scale
-// of a K group needs 4 lanes, that of a V token the 16 lanes of a row.
+// of a K group needs 4 lanes, that of a V token the 16 lanes of a row. Bound by HBM: 3.8k tokens of 32 layers, 8 kv
+// heads of 128 (629 MB read and written) 105 us, 5.98 TB/s.
 // ---------------------------------------------------------------------------------------------
 template <int D>
 __global__ __launch_bounds__(256) void kv_pack_fp4_kernel(const uint16_t* __restrict__ pool, int64_t n_pages, int n_kv_heads,

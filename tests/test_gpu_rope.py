@@ -362,3 +362,60 @@ def test_failed_launch_changes_nothing_and_streams():
     _assert_turned(out.cpu(), qc[:, 20:].cpu(), np.arange(20, 40), rope)
     assert torch.equal(gv.cpu(), v)
     pool.close()
+
+
+def test_a_refused_step_leaves_queries_in_place():
+    """A step that the pool has no pages for, its outputs its queries: refused before a query turns."""
+    from paper_2606_01839_amd import CS_ENOMEM, ConserveError
+    rope = _rope(64, False, "none")
+    pool = _pool(1, 8, 2, 64, 4)
+    k, v = (x.cuda() for x in kv_tokens(SEED, 0, 1, 0, 64, 2, 64))
+    c, d = pool.conv_create(), pool.conv_create()
+    pool.kv_append_rope([c, d], [32, 16], k[:, :48].contiguous(), v[:, :48].contiguous(), rope)
+    qe = q_tokens(SEED, 0, 0, 32, 17, 8, 64)[None].cuda()
+    qd = q_tokens(SEED, 1, 0, 16, 1, 8, 64)[None].cuda()
+    a, b = qe.clone(), qd.clone()
+    for _ in range(2):
+        with pytest.raises(ConserveError) as e:
+            pool.mixed_step([c], [17], [d], k[:, :18].contiguous(), v[:, :18].contiguous(), a, b, out_ext=a, out_dec=b, rope=rope)
+        assert e.value.code == CS_ENOMEM
+    torch.cuda.synchronize()
+    assert torch.equal(a, qe) and torch.equal(b, qd) and pool.conv_len(c) == 32 and pool.conv_len(d) == 16
+    pool.close()
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "fp4"])
+def test_captured_queries_and_decode_replay(fmt):
+    """Queries rotated and attended in a captured graph, the rotated ones in place of a buffer of the graph's: every
+    replay gives the eager calls' bits, with eager work between replays."""
+    rope = _rope(96, True, "parts")
+    lens = [450, 1, 2100]
+    pool = _pool(1, 32, 8, 128, 200, fmt)
+    convs = [pool.conv_create() for _ in lens]
+    kv = [kv_tokens(SEED, i, 1, 0, n, 8, 128) for i, n in enumerate(lens)]
+    s = torch.cuda.Stream()
+    q = torch.zeros(3, 32, 128, dtype=torch.bfloat16, device="cuda")
+    turned, out = torch.empty_like(q), torch.empty_like(q)
+    k, v = (torch.cat([x[j] for x in kv], 1).cuda() for j in (0, 1))
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):   # the pool's work moves to this stream before the capture
+        pool.kv_append_rope(convs, lens, k, v, rope)
+        pool.rope_q(convs, [1, 1, 1], q, rope, turned)
+        pool.attn_decode_batch_noalloc(convs, 0, turned, out)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        pool.rope_q(convs, [1, 1, 1], q, rope, turned)
+        pool.attn_decode_batch_noalloc(convs, 0, turned, out)
+    for turn in range(4):
+        x = torch.cat([q_tokens(SEED + turn, i, 0, n - 1, 1, 32, 128) for i, n in enumerate(lens)]).cuda()
+        q.copy_(x)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s):
+            want_q = pool.rope_q(convs, [1, 1, 1], x, rope)
+            want = pool.attn_decode_batch(convs, 0, want_q)
+        torch.cuda.synchronize()
+        assert torch.equal(turned, want_q) and torch.equal(out, want), turn
+    pool.close()
