@@ -534,7 +534,8 @@ struct DecodeWork {
 
 cs::DecodePlan plan_decode_batch(const cs_pool* p, const std::vector<int32_t>& slots,
                                  const std::vector<int64_t>& lens) {
-  return cs::plan_decode_filling(slots, lens, p->desc.n_kv_heads, kDecodeTargetItems, cs::kCus);
+  return p->fp4 ? cs::plan_decode_rounds(slots, lens, p->desc.n_kv_heads, kDecodeTargetItems, cs::kCus)
+                : cs::plan_decode_filling(slots, lens, p->desc.n_kv_heads, kDecodeTargetItems, cs::kCus);
 }
 
 // Descriptors and launch order of a decode plan, as laid out back to back.

@@ -121,18 +121,32 @@ DecodePlan plan_decode(const std::vector<int32_t>& slots, const std::vector<int6
   return decode_plan_of(slots, lens, split);
 }
 
+// Work items of splits of `split` keys, over all kv heads.
+static int64_t decode_workgroups(const std::vector<int64_t>& lens, int32_t n_kv_heads, int32_t split) {
+  const int64_t item_keys = static_cast<int64_t>(kDecodeSubSplits) * split;
+  int64_t items = 0;
+  for (int64_t L : lens) items += (L + item_keys - 1) / item_keys;
+  return items * n_kv_heads;
+}
+
 DecodePlan plan_decode_filling(const std::vector<int32_t>& slots, const std::vector<int64_t>& lens,
                                int32_t n_kv_heads, int64_t target_items, int32_t n_cus) {
   DecodePlan plan = plan_decode(slots, lens, n_kv_heads, target_items);
   if (static_cast<int64_t>(plan.n_items) * n_kv_heads >= n_cus) return plan;
   for (const DecodeConvDesc& c : plan.convs)
     if (c.n_splits < 2) return plan;
-  for (int32_t split = 32; split < plan.split_tokens; split += 32) {
-    int64_t items = 0;
-    const int64_t item_keys = static_cast<int64_t>(kDecodeSubSplits) * split;
-    for (int64_t L : lens) items += (L + item_keys - 1) / item_keys;
-    if (items * n_kv_heads <= n_cus) return decode_plan_of(slots, lens, split);
-  }
+  for (int32_t split = 32; split < plan.split_tokens; split += 32)
+    if (decode_workgroups(lens, n_kv_heads, split) <= n_cus) return decode_plan_of(slots, lens, split);
+  return plan;
+}
+
+DecodePlan plan_decode_rounds(const std::vector<int32_t>& slots, const std::vector<int64_t>& lens,
+                              int32_t n_kv_heads, int64_t target_items, int32_t n_cus) {
+  DecodePlan plan = plan_decode_filling(slots, lens, n_kv_heads, target_items, n_cus);
+  if (static_cast<int64_t>(plan.n_items) * n_kv_heads <= n_cus) return plan;
+  for (int32_t rounds = 1; rounds <= 2; ++rounds)
+    for (int32_t split = plan.split_tokens + 32; split <= (rounds == 1 ? 512 : 384); split += 32)
+      if (decode_workgroups(lens, n_kv_heads, split) <= rounds * n_cus) return decode_plan_of(slots, lens, split);
   return plan;
 }
 
