@@ -9,6 +9,8 @@ tokens and reuse the cached prefix; the turn-1 cache is moved once to the decode
   (no pages), for turn-1 prefill, extend and decode queries.
 * ``oracle.kvwire`` -- the conversation KV store as plain concatenation, and the wire format of the
   one-time KV transfer (serialize / deserialize).
+* ``oracle.fp4`` -- the 4-bit values of a cache, their scales and the 4-bit wire format.
+* ``oracle.rope`` -- rotary positions: frequencies and the rotation of pairs.
 
 Only ``tests/``, ``__graft_entry__.smoke()`` and the CPU-baseline leg of ``bench.py`` may import this
 package. It shares no code with the HIP library (``paper_2606_01839_amd``) and imports nothing from

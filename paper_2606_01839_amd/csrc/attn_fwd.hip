@@ -31,6 +31,9 @@
 // 128; a library product of 8192^3 reaches 1.37). Small ones by a workgroup's start-up, 9 us at head dim
 // 128 of which 0.5 is the plan, 1.5 pages, queries and first copies, 1.0 their arrival, 2.5 the first
 // tile (mask, weights taken twice) and 2.0-3.7 were 8-byte output stores into 32 rows at a time.
+// Over 4-bit pages (fp4.hpp) a launch is bound by the same, with 3/4 of the score product's matrix time and the conversion
+// of V beside it: eight conversations' 128-2048 tokens on 8k-40k 1451-1525 us (1.20-1.26 PFLOP/s; bf16 pages 1598), 301
+// tokens on 41k 175-182 (217); at head dim 64 the softmax leaves no difference (111 us against 109).
 // Head dim 64 against a kernel that staged tiles through registers, one wave per SIMD: six prompts of
 // 300-9000 tokens 361 -> 229 us.
 #include <cfloat>

@@ -307,7 +307,7 @@ __global__ __launch_bounds__(256) void rope_q_kernel(LaunchMeta, RopeArgs rope, 
 
 // ---------------------------------------------------------------------------------------------
 // Read back: one wave per (chunk, layer, kv head); V through LDS into token rows. Bound by HBM: 12.5k tokens of 32
-// layers, 8 kv heads of 128 out of 4-bit pages (2.09 GB read and written) 377 us, 5.54 TB/s; 5.3k out of bf16 pages (1.39 GB)
+// layers, 8 kv heads of 128 out of 4-bit pages (2.09 GB read and written) 382 us, 5.47 TB/s; 5.3k out of bf16 pages (1.39 GB)
 // 243 us, 5.73 TB/s (283 with the K loads behind the V part and the cached forms).
 // ---------------------------------------------------------------------------------------------
 template <int D, bool FP4>
