@@ -228,6 +228,31 @@ def test_decode(hq, hkv, d):
     pool.close()
 
 
+@pytest.mark.parametrize("hq,hkv,d,lens", [
+    (32, 8, 128, [40003]),                                                  # longer items in one round of the CUs
+    (32, 8, 64, [1000 + 37 * i * i for i in range(15)]),                    # ragged ones
+    (32, 8, 128, [300 + 27 * i for i in range(64)]),                        # two rounds, a single item each
+    (64, 8, 128, [9000 - 7 * i for i in range(9)]),
+])
+def test_decode_in_whole_rounds(hq, hkv, d, lens):
+    """Batches whose items the plan of 4-bit pools makes longer: alone on the workspace and on the static records,
+    and a part of the batch, whose plan is another."""
+    pool = _pool(1, hq, hkv, d, sum(lens) // 16 + 80, max_convs=len(lens), max_pages=max(lens) // 16 + 2)
+    convs, kv = _fill(pool, 1, lens, hkv, d)
+    q = torch.cat([q_tokens(SEED, i, 0, n - 1, 1, hq, d) for i, n in enumerate(lens)])
+    out = pool.attn_decode_batch(convs, 0, q.cuda())
+    again = pool.attn_decode_batch_noalloc(convs, 0, q.cuda(), torch.full_like(out, float("nan")))
+    part = sorted({0, 1, len(lens) // 2, len(lens) - 1} & set(range(len(lens))))
+    alone = pool.attn_decode_batch([convs[i] for i in part], 0, q[part].contiguous().cuda())
+    torch.cuda.synchronize()
+    assert torch.equal(out, again)
+    for r, i in enumerate(part):
+        ref = attend_last(f64(q[i:i + 1]), *[x[0] for x in _held(*kv[i])])
+        assert_close(out[i:i + 1], ref, f"decode of {lens[i]} in the batch")
+        assert_close(alone[r:r + 1], ref, f"decode of {lens[i]}")
+    pool.close()
+
+
 @pytest.mark.parametrize("hq,hkv,d", SHAPES)
 def test_extend_and_prefill(hq, hkv, d):
     """Chunks of 0 .. all tokens in one launch, whole tiles and pieces, padding rows of a query tile."""
