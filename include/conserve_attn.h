@@ -199,7 +199,7 @@ cs_status cs_rope_init(cs_rope* out, int32_t rotary_dim, int32_t interleaved, do
 /*
  * cs_kv_append_batch with rotated keys: a token's K enters the cache turned by its position. With q (may be
  * null) the queries of the same tokens, [n_layers][sum(n_new)][n_q_heads][head_dim], are rotated in the same
- * launch into q_out (same shape; q itself, or no overlap with it), ready for the attention calls.
+ * call into q_out (same shape; q itself, or no overlap with it), ready for the attention calls.
  * Errors: as cs_kv_append_batch; CS_EINVAL for a null or invalid rope (rotary_dim no multiple of 16 in
  * 16 .. head_dim, interleaved not 0 or 1, amplitude or an inv_freq in use not finite), q without q_out, q of more
  * than 2^28 - 16 rows. After CS_EHIP q_out is undefined: queries rotated in place may or may not have turned.

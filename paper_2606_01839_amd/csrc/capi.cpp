@@ -677,10 +677,12 @@ cs_status run_rope_q(cs_pool* p, const std::vector<cs::RopeConv>& convs, int64_t
   return st;
 }
 
-// An append rotates more query bytes than this in a launch of their own (5300 tokens, 32 layers, 32 query heads,
-// 1.4 GB: 764 us in two launches, 803 in one, whose workgroups of queries share a CU with the LDS of the K and
-// V's); below, one launch saves the other's start (64 single tokens of 32 layers, 17 MB).
-constexpr size_t kRopeApartBytes = size_t(64) << 20;
+// An append whose queries would take more workgroups than this rotates them in a launch of their own: the other's
+// share a CU with the LDS of the K and V's (5300 tokens, 32 layers, 32 query heads, 1.4 GB: 764 us in two launches, 803 in
+// one), and take page by page what this one takes row by row (64 single tokens of 32 layers: 39 us against 72).
+// Up to it one launch saves the other's start (300 tokens of one layer 13.5 us against 15.8, two times 64 tokens of 32
+// layers 21.1 against 28.3).
+constexpr int64_t kRopeApartGroups = 512;
 
 // `rotated` (may be null): keys turn on their way into the pages, and the queries with them.
 cs_status append_impl(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t* n_new,
@@ -727,8 +729,7 @@ cs_status append_impl(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t
 
   const cs::PoolGeom g = p->geom();
   const size_t carry_bytes = carry ? carry->bytes.size() : 0;
-  const bool q_apart = rotated && rotated->q &&
-                       static_cast<size_t>(total) * g.n_layers * g.n_q_heads * g.head_dim * 2 > kRopeApartBytes;
+  const bool q_apart = rotated && rotated->q && cs::append_rope_groups(g, chunks.size()) > kRopeApartGroups;
   auto launch = [&](const cs::Meta& m, int n_chunks, const cs::AppendCarry& c) {
     return timed_launch(p, CS_PROF_APPEND, "append launch", [&] {
       if (rotated)

@@ -79,7 +79,9 @@ struct RopeConv {
 hipError_t launch_rope_q(const PoolGeom& g, const Meta& meta, int n_convs, int64_t rows, int n_layers, const RopeArgs& rope,
                          const void* q, void* out, hipStream_t stream);
 
-// Layers one such launch may take (a grid dimension).
+// Workgroups that the queries of an append of n_chunks add to its launch.
+int64_t append_rope_groups(const PoolGeom& g, size_t n_chunks);
+// Layers one launch_rope_q may take (a grid dimension).
 int rope_q_layers(const PoolGeom& g);
 
 // Read back: chunks (meta: PageChunk[n_chunks]) of the pool to k, v [n_layers][dst_rows][Hkv][D] in bf16.

@@ -584,6 +584,10 @@ hipError_t launch_append_as(const PoolGeom& g, const Meta& meta, int n_chunks, c
   });
 }
 
+int64_t append_rope_groups(const PoolGeom& g, size_t n_chunks) {
+  return static_cast<int64_t>((n_chunks + kChunks - 1) / kChunks) * g.n_layers * ((g.n_q_heads + kQHeads - 1) / kQHeads);
+}
+
 int rope_q_layers(const PoolGeom& g) { return std::max(1, 65535 / ((g.n_q_heads + kQHeads - 1) / kQHeads)); }
 
 hipError_t launch_rope_q(const PoolGeom& g, const Meta& meta, int n_convs, int64_t rows, int n_layers, const RopeArgs& rope,

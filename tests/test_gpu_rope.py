@@ -215,6 +215,30 @@ def test_large_appends_are_uploaded_in_parts():
     pool.close()
 
 
+@pytest.mark.parametrize("n,nl", [(7, 2), (64, 20)])
+def test_single_tokens_of_many_conversations(n, nl):
+    """One token each, its queries in the append's launch (few) or in one of their own (many): the bits of rope_q, in
+    place too, and the oracle's."""
+    rope = _rope(48, True, "linear")
+    pool = _pool(nl, 32, 4, 64, 600, max_convs=n)
+    lens = [3 * i for i in range(n)]
+    convs = [pool.conv_create() for _ in range(n)]
+    k, v = (x.cuda() for x in kv_tokens(SEED, 0, nl, 0, sum(lens) + 2 * n, 4, 64))
+    pool.kv_append_rope(convs, lens, k[:, :sum(lens)].contiguous(), v[:, :sum(lens)].contiguous(), rope)
+    for step in range(2):
+        at = slice(sum(lens) + step * n, sum(lens) + (step + 1) * n)
+        x = torch.stack([q_tokens(SEED + step, 0, l, 0, n, 32, 64) for l in range(nl)])
+        q = x.cuda()
+        out = pool.kv_append_rope(convs, [1] * n, k[:, at].contiguous(), v[:, at].contiguous(), rope, q=q, q_out=q if step else None)
+        again = pool.rope_q(convs, [1] * n, x.cuda(), rope)
+        gk, gv = pool.kv_read(convs, [m + step for m in lens], [1] * n)
+        torch.cuda.synchronize()
+        assert torch.equal(out, again) and torch.equal(gv, v[:, at])
+        _assert_turned(out.cpu(), x, np.array(lens) + step, rope)
+        _assert_turned(gk.cpu(), k[:, at].cpu(), np.array(lens) + step, rope)
+    pool.close()
+
+
 @pytest.mark.parametrize("fmt", ["bf16", "fp4"])
 @pytest.mark.parametrize("hq,hkv,d,r", [(32, 8, 128, 128), (4, 2, 64, 32)])
 def test_a_served_conversation(fmt, hq, hkv, d, r):
