@@ -210,8 +210,8 @@ cs_status cs_kv_append_rope(cs_pool* pool, const cs_rope* rope, int32_t n_convs,
 /*
  * Queries of the last q_lens[i] positions of each conversation (those the attention calls take), rotated:
  * q, out [n_layers][sum(q_lens)][n_q_heads][head_dim] for any n_layers >= 0; out may be q itself, otherwise
- * they do not overlap. Errors: as cs_attn_extend, and as cs_kv_append_rope for rope and after CS_EHIP; CS_EINVAL
- * (n_layers < 0, more than 2^28 - 16 rows).
+ * they do not overlap. May be captured into a graph, as cs_attn_decode_batch_noalloc. Errors: as cs_attn_extend,
+ * and as cs_kv_append_rope for rope and after CS_EHIP; CS_EINVAL (n_layers < 0, more than 2^28 - 16 rows).
  */
 cs_status cs_rope_q(cs_pool* pool, const cs_rope* rope, int32_t n_convs, const cs_conv* convs, const int32_t* q_lens,
                     int32_t n_layers, const void* q, void* out, cs_stream stream);
@@ -277,6 +277,9 @@ cs_status cs_attn_decode_batch(cs_pool* pool, int32_t n_convs, const cs_conv* co
  * untimed: cs_profile_* does not see it.
  * Every call on one GPU shares that GPU's array: calls that overlap on one GPU (on different
  * streams, or from different pools on different host threads) race and must not be issued.
+ * Captured into a graph, the batch's descriptors are part of the graph, of whatever size. A replay is work
+ * of the pool: it must not overlap the pool's other calls or another graph's replay, and it decodes at the
+ * lengths that the conversations had at the capture.
  * Errors: as cs_attn_decode_batch; CS_ENOMEM when the batch's partial records
  * (n_items * n_q_heads * (head_dim + 4) floats; batches whose conversations are each one work item
  * need none) exceed the array; CS_ESTATE when the pool has made no device call yet (its first one

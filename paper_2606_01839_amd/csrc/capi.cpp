@@ -107,7 +107,7 @@ struct cs_pool {
   bool dev_ready = false;
   int device = -1;
   char* h_ring = nullptr;
-  size_t ring_head = 0;
+  size_t ring_head = 0, capture_head = 0;
   int cur_quarter = -1;
   hipEvent_t quarter_ev[4] = {};
   bool quarter_used[4] = {};
@@ -305,16 +305,21 @@ cs_status ensure_side(cs_pool* p) {
 // Reserve `n` bytes of the metadata ring inside one quarter. Entering a quarter records an event
 // closing the previous one (everything enqueued so far) and waits for the event that closed the
 // entered quarter last time round, so a region is never rewritten while a copy or kernel of an
-// earlier call may still read it.
-cs_status ring_reserve(cs_pool* p, size_t n, size_t* off_out) {
+// earlier call may still read it. Under stream capture (*captured) only the ring's device half is
+// used, which the pool's work reads and writes in stream order: no events, and a head of its own.
+cs_status ring_reserve(cs_pool* p, size_t n, size_t* off_out, bool* captured) {
   n = align_up(std::max<size_t>(n, 1), kAlign);
   if (n > kQuarter) return fail(CS_ENOMEM, "metadata for one launch exceeds the upload ring");
-  size_t off = p->ring_head;
+  hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+  CS_HIP(hipStreamIsCapturing(p->stream, &cap), "hipStreamIsCapturing");
+  *captured = cap != hipStreamCaptureStatusNone;
+  size_t& head = *captured ? p->capture_head : p->ring_head;
+  size_t off = head;
   if (off / kQuarter != (off + n - 1) / kQuarter || off + n > kRingBytes)
     off = ((off + kQuarter - 1) / kQuarter) * kQuarter;
   if (off + n > kRingBytes) off = 0;
   const int q = static_cast<int>(off / kQuarter);
-  if (q != p->cur_quarter) {
+  if (!*captured && q != p->cur_quarter) {
     if (p->cur_quarter >= 0) {
       CS_HIP(hipEventRecord(p->quarter_ev[p->cur_quarter], p->stream), "hipEventRecord");
       p->quarter_used[p->cur_quarter] = true;
@@ -322,19 +327,26 @@ cs_status ring_reserve(cs_pool* p, size_t n, size_t* off_out) {
     if (p->quarter_used[q]) CS_HIP(hipEventSynchronize(p->quarter_ev[q]), "hipEventSynchronize");
     p->cur_quarter = q;
   }
-  p->ring_head = off + n;
+  head = off + n;
   *off_out = off;
   return CS_OK;
 }
 
-// Copy host bytes into the ring and enqueue their upload; returns the device address.
+// Copy host bytes into the ring and enqueue their upload; returns the device address. A captured copy would
+// read the ring's host half again at every replay, when later calls have written over it: there the bytes
+// travel in launch arguments, which the graph keeps.
 cs_status upload(cs_pool* p, const void* src, size_t n, void** dev_out) {
   size_t off = 0;
-  cs_status st = ring_reserve(p, n, &off);
+  bool captured = false;
+  cs_status st = ring_reserve(p, n, &off, &captured);
   if (st != CS_OK) return st;
-  std::memcpy(p->h_ring + off, src, n);
   char* d = p->ws + p->lay.ring + off;
-  CS_HIP(hipMemcpyAsync(d, p->h_ring + off, n, hipMemcpyHostToDevice, p->stream), "hipMemcpyAsync");
+  if (captured) {
+    CS_HIP(cs::launch_store_meta(src, n, d, p->stream), "metadata launch");
+  } else {
+    std::memcpy(p->h_ring + off, src, n);
+    CS_HIP(hipMemcpyAsync(d, p->h_ring + off, n, hipMemcpyHostToDevice, p->stream), "hipMemcpyAsync");
+  }
   *dev_out = d;
   return CS_OK;
 }
@@ -747,7 +759,8 @@ cs_status append_impl(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t
     cs::AppendCarry c;
     if (carry_bytes > 0) {
       size_t off = 0;
-      st = ring_reserve(p, carry_bytes, &off);
+      bool captured = false;   // (the append kernel stores it either way)
+      st = ring_reserve(p, carry_bytes, &off, &captured);
       c.dst = p->ws + p->lay.ring + off;
       c.bytes = carry_bytes;
       c.off = b.push(carry->bytes.data(), carry_bytes);

@@ -47,6 +47,10 @@ inline void fill_meta(const Meta& m, LaunchMeta* out) {
   if (m.dev == nullptr) std::memcpy(out->w, m.host, m.bytes);
 }
 
+// Metadata to device memory (16-byte aligned, room up to a multiple of 16) in the arguments of launches,
+// kMetaBytes each: what a captured graph keeps, unlike a copy's source.
+hipError_t launch_store_meta(const void* host, size_t bytes, void* dst, hipStream_t stream);
+
 // KV append: write chunks (meta: PageChunk[n_chunks]) of k,v [n_layers][src_rows][Hkv][D]. With
 // carry_bytes > 0 the metadata travels in the kernel arguments and its bytes [carry_off, carry_off +
 // carry_bytes) (multiples of 16) are also stored to carry_dst, for the launches that follow.

@@ -112,6 +112,16 @@ __global__ __launch_bounds__(256) void kv_append_kernel(LaunchMeta, const void* 
   }
 }
 
+// The first 16 n16 bytes of the launch's arguments to dst.
+__global__ __launch_bounds__(kMetaBytes / 16) void store_meta_kernel(LaunchMeta, uint4* __restrict__ dst, int n16) {
+  const auto* src = meta_at<u32x4_t>(nullptr, 0);
+  const int i = threadIdx.x;
+  if (i < n16) {
+    const u32x4_t x = src[i];
+    dst[i] = make_uint4(x.x, x.y, x.z, x.w);
+  }
+}
+
 // Zero the token slots >= valid inside 16-byte chunk i (8 elements) of a block.
 template <int D>
 __device__ __forceinline__ uint4 mask_tail(uint4 x, int i, int valid) {
@@ -193,6 +203,18 @@ static hipError_t by_dim(int D, F&& f) {
   if (D == 64) return f(std::integral_constant<int, 64>{});
   if (D == 128) return f(std::integral_constant<int, 128>{});
   return hipErrorInvalidValue;
+}
+
+hipError_t launch_store_meta(const void* host, size_t bytes, void* dst, hipStream_t stream) {
+  for (size_t at = 0; at < bytes; at += kMetaBytes) {
+    const size_t n = bytes - at < kMetaBytes ? bytes - at : kMetaBytes;
+    LaunchMeta m{};
+    std::memcpy(m.w, static_cast<const char*>(host) + at, n);
+    store_meta_kernel<<<1, kMetaBytes / 16, 0, stream>>>(m, reinterpret_cast<uint4*>(static_cast<char*>(dst) + at),
+                                                         static_cast<int>((n + 15) / 16));
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 hipError_t launch_append(const PoolGeom& g, const Meta& meta, int n_chunks, const AppendCarry& carry,
