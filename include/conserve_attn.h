@@ -107,12 +107,13 @@ cs_status cs_pool_create(const cs_pool_desc* desc, void* kv_base, size_t kv_byte
  *   dims of a token and kv head, for V one for every token and kv head. With a the largest magnitude of
  *   such a group the power is 2^(floor(log2 a) - 2), at least 2^-126; a value is rounded to the nearest
  *   e2m1 value times it (ties to the even code) and at most to 6 times it. K and V must be finite: a group
- *   with an infinity or NaN reads back as NaN. Attention is that of the held values: every call below does on
- *   such a pool what it does on a bf16 one, with the same arguments, asynchrony and errors.
+ *   with an infinity or NaN is held, read back and attended as NaN. Attention is that of the held values:
+ *   every call below does on such a pool what it does on a bf16 one, with the same arguments, asynchrony and
+ *   errors.
  *   Block (layer, page, kv head), two codes a byte, the first in the low bits: K[d/32 groups][16 tokens][32
  *   dims], V[4][16][d/16][4]: part i, row c, tile t hold dim 16 t + c of tokens 4 i .. 4 i + 3; then bytes e
- *   (the power 2^(e - 127)): K[16 tokens][d/32 groups], V[16 tokens], zeros up to 17 d. Token slots >= length
- *   are zeros.
+ *   (the power 2^(e - 127); 255: NaN, V's codes then zeros): K[16 tokens][d/32 groups], V[16 tokens], zeros
+ *   up to 17 d. Token slots >= length are zeros.
  */
 enum { CS_KV_BF16 = 0, CS_KV_FP4 = 1 };
 

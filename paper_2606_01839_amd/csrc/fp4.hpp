@@ -43,7 +43,8 @@ struct Fp4Block {
 
 // The scale byte of a group whose largest magnitude has the given fp32 bits (sign cleared): the power of
 // two floor(log2 a) - 2, so that a / scale lies in [4, 8) and e2m1's largest value, 6, is reached; at
-// least 2^-126. A group with an infinity or NaN gets 255, which reads back as NaN.
+// least 2^-126. A group with an infinity or NaN gets 255, which reads back as NaN; of V its codes are zeros,
+// so that the decode's weight times that scale, an infinity, gives NaN with them too.
 __device__ __forceinline__ uint32_t fp4_scale_byte(uint32_t abs_bits) {
   const int e = static_cast<int>(abs_bits >> 23);
   return e == 255 ? 255u : static_cast<uint32_t>(max(e - 2, 1));

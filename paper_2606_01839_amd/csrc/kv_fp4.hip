@@ -195,7 +195,7 @@ __global__ __launch_bounds__(256) void kv_append_as_kernel(LaunchMeta, RopeArgs 
         }
         unpack8(vv[i][ps], x);
         const uint32_t vb = fp4_scale_byte(group_max<kCh>(max_bits(x)));
-        vts[wave][i][t][ch] = fp4_encode8(x, fp4_scale(vb));
+        vts[wave][i][t][ch] = vb == 255 ? 0u : fp4_encode8(x, fp4_scale(vb));
         if (writes && ch == 0) blk[B::kVScale + t] = static_cast<uint8_t>(in ? vb : 0);
       } else {
         if (writes) st16(blk16 + k_elem(t, ch), ROPE ? pack8(x) : kv[i][ps]);
@@ -502,12 +502,13 @@ __global__ __launch_bounds__(256) void kv_pack_fp4_kernel(const uint16_t* __rest
     vm[2] = dpp_max(vm[2], abs_bits(bf16_lo(vx[t].y)));
     vm[3] = dpp_max(vm[3], abs_bits(bf16_hi(vx[t].y)));
   }
-  uint32_t vb = 0;
+  uint32_t vb = 0, held = 0;
   float inv[4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     const uint32_t b = fp4_scale_byte(group_max<16>(vm[k]));
     vb |= (4 * qd + k < valid ? b : 0u) << (8 * k);
+    held |= (b == 255 ? 0u : 0x000F000Fu) << (4 * k);
     inv[k] = fp4_scale(254 - min(b, 253u));   // exact: 1 / scale
   }
   uint32_t vw[NW];
@@ -516,7 +517,7 @@ __global__ __launch_bounds__(256) void kv_pack_fp4_kernel(const uint16_t* __rest
     const uint2 a = vx[2 * j], b = vx[2 * j + 1];
     const float x[8] = {bf16_lo(a.x) * inv[0], bf16_hi(a.x) * inv[1], bf16_lo(a.y) * inv[2], bf16_hi(a.y) * inv[3],
                         bf16_lo(b.x) * inv[0], bf16_hi(b.x) * inv[1], bf16_lo(b.y) * inv[2], bf16_hi(b.y) * inv[3]};
-    vw[j] = fp4_encode8(x, 1.f);
+    vw[j] = fp4_encode8(x, 1.f) & held;
   }
 #pragma unroll
   for (int i = 0; i < NW; ++i) *reinterpret_cast<uint32_t*>(dst + B::kK + 256 * i + 4 * lane) = kw[i];
