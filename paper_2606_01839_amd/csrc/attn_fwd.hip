@@ -83,6 +83,10 @@ static_assert(kBN == kExtendKeyTile, "the plan counts the kernel's key tiles");
 
 // Per-lane bound on the sum of a tile's weights (32 keys per lane) before the max is refreshed.
 constexpr float kSumLimit = 256.f;
+// A score times c minus the maximum as one fused operation is exact but for the maximum's own rounding, the same for
+// every weight of a row: for scores past 2^31 half a step of the maximum, 2^7 and more, whose power of two is an
+// infinity. From here on (fp32 steps of 1 and more) both are rounded before they are subtracted, so the largest weight is 1.
+constexpr float kFarScore = 0x1p23f;
 
 // ------------------------------------------------------------------------------------------------
 // K/V copied from HBM straight into LDS.
@@ -129,7 +133,7 @@ __device__ __forceinline__ void lds_wait_barrier() { asm volatile("s_waitcnt lgk
 //
 // PRE: the K operands of the next tile and the V operands of this one are read from LDS ahead of the
 // matrix instructions that use them (two waves per SIMD have little else to cover the LDS latency).
-// Without it a head_dim 64 wave needs 121 registers and two workgroups fit a CU.
+// Without it a head_dim 64 wave needs 116 to 120 registers (4-bit pages: 126 to 128) and two workgroups fit a CU.
 // CHAIN: tiles may hold pieces to take one after the other (a form of its own, since the code around
 // the loop costs launches without such tiles 1.5%).
 //
@@ -342,6 +346,7 @@ __device__ __forceinline__ void attn_fwd_block(const ExtendArgs& a, const int bl
   // score but that value itself, so a row's first visible tile always refreshes it, and a row that
   // sees no key of a piece's first tiles keeps weights of 0 (no inf - inf).
   float m_s = -FLT_MAX, l_run = 0.f;
+  bool far = false;   // a row's maximum is past kFarScore
   const bf16x2 ones = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
 
   // Start of a step: the tile three (4-bit pages: two) ahead goes on its way into the ring.
@@ -471,9 +476,9 @@ __device__ __forceinline__ void attn_fwd_block(const ExtendArgs& a, const int bl
     // Weights against the running max m. If a lane's partial sum over its 32 keys of the tile
     // exceeds 2^8 or is not finite (always on a row's first visible tile), the wave takes the
     // tile's row max, rescales O and l and recomputes the weights: every weight stays <= 2^8
-    // without a max reduction on the common path.
+    // without a max reduction on the common path. Maxima past kFarScore take the other path always.
     bf16x8 pop[2][2];
-    auto weights = [&](float neg_m) {
+    auto weights = [&](float c, float neg_m) {
       float ps0 = 0.f, ps1 = 0.f;
 #pragma unroll
       for (int kt2 = 0; kt2 < 2; ++kt2) {
@@ -496,8 +501,8 @@ __device__ __forceinline__ void attn_fwd_block(const ExtendArgs& a, const int bl
       }
       return ps0 + ps1;
     };
-    float ps = weights(-m_s);
-    if (__builtin_amdgcn_ballot_w64(!(ps <= kSumLimit)) != 0) {
+    float ps = weights(c, -m_s);
+    if (far || __builtin_amdgcn_ballot_w64(!(ps <= kSumLimit)) != 0) {
       float mx = -INFINITY;
 #pragma unroll
       for (int kt2 = 0; kt2 < 2; ++kt2)
@@ -509,7 +514,19 @@ __device__ __forceinline__ void attn_fwd_block(const ExtendArgs& a, const int bl
       l_run *= alpha;
 #pragma unroll
       for (int t = 0; t < DT; ++t) o[t] *= alpha;
-      ps = weights(-m_new);
+      float w_scale = c, w_off = -m_new;
+      // (-FLT_MAX: a row that has seen no key)
+      far = __builtin_amdgcn_ballot_w64(m_new > -FLT_MAX && __builtin_fabsf(m_new) >= kFarScore) != 0;
+      if (far) {
+#pragma clang fp contract(off)
+#pragma unroll
+        for (int kt2 = 0; kt2 < 2; ++kt2)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[kt2][e] = s[kt2][e] * c - m_new;
+        w_scale = 1.f;
+        w_off = 0.f;
+      }
+      ps = weights(w_scale, w_off);
     }
     l_run += ps;
 #pragma unroll

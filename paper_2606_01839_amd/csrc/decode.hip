@@ -66,7 +66,7 @@ __global__ __launch_bounds__(kDecodeItemThreads) void decode_split_kernel(Launch
 }
 
 // the same over 4-bit pages. Held to 128 registers: two workgroups a CU hide the arithmetic between a page's arrival
-// and its weights (122 and 115 are used; with 160, one workgroup a CU and more pages in flight, one conversation of 100k
+// and its weights (122 and 116 are used; with 160, one workgroup a CU and more pages in flight, one conversation of 100k
 // tokens takes 26.0 us instead of 24.0).
 template <int D>
 __global__ __launch_bounds__(kDecodeItemThreads) __attribute__((amdgpu_waves_per_eu(4))) void decode_split_fp4_kernel(LaunchMeta, DecodeArgs a) {

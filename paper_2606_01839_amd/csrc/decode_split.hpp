@@ -175,9 +175,11 @@ __device__ __forceinline__ void split_body(const DecodeArgs& a, const int work, 
       for (int r = 1; r < 8; ++r) mx = fmaxf(mx, x[r]);
       mx = fmaxf(mx, xor_shfl(mx, 16));
       mx = fmaxf(mx, xor_shfl(mx, 32));
-      const float m_new = fmaxf(m_run, mx * a.scale_log2);
+      // The running maximum is subtracted before the scale is applied: of scores past 2^31 a fused x scale - m, m rounded,
+      // is up to half a step of m (2^7 and more) above 0 for the largest, whose weight would be an infinity.
+      const float m_new = fmaxf(m_run, mx);
       if (__builtin_amdgcn_ballot_w64(!(m_new <= m_run)) != 0) {
-        const float alpha = fast_exp2(m_run - m_new);
+        const float alpha = fast_exp2((m_run - m_new) * a.scale_log2);
         m_run = m_new;
         l_run *= alpha;
 #pragma unroll
@@ -185,7 +187,7 @@ __device__ __forceinline__ void split_body(const DecodeArgs& a, const int work, 
       }
       float p[8];
 #pragma unroll
-      for (int r = 0; r < 8; ++r) p[r] = fast_exp2(__builtin_fmaf(x[r], a.scale_log2, -m_run));
+      for (int r = 0; r < 8; ++r) p[r] = fast_exp2((x[r] - m_run) * a.scale_log2);
       const uint4 pw = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
       // The denominator sums the same bf16-rounded weights the PV product uses: scaling by the values' power
       // of two commutes with the rounding.
@@ -231,6 +233,7 @@ __device__ __forceinline__ void split_body(const DecodeArgs& a, const int work, 
         step(pa, pb, j, query);
       }
     }
+    if (n_pg > 0) m_run *= a.scale_log2;
   } else {
     const size_t head_stride = static_cast<size_t>(2 * kPageTokens * D);
     const uint16_t* layer_base = a.pool + static_cast<size_t>(a.layer + dl) * a.n_pages * a.n_kv_heads * head_stride +
