@@ -1135,10 +1135,16 @@ static cs_status pack_impl(const cs_pool* pc, cs_conv conv, bool fp4, void* dst,
   cs_status st;
   if ((st = ensure_device(p)) != CS_OK) return st;
   if ((st = use_stream(p, as_stream(stream))) != CS_OK) return st;
-  return timed_launch(p, CS_PROF_PACK, "pack launch", [&] {
-    return fp4 ? cs::launch_pack_fp4(p->geom(), cs::ConvTable::slot_of(conv), c->len, dst, p->stream)
-               : cs::launch_pack(p->geom(), cs::ConvTable::slot_of(conv), c->len, dst, p->stream);
-  });
+  const int slot = cs::ConvTable::slot_of(conv);
+  if (!fp4)
+    return timed_launch(p, CS_PROF_PACK, "pack launch",
+                        [&] { return cs::launch_pack(p->geom(), slot, c->len, dst, p->stream); });
+  const int n_pages = static_cast<int>(cs::pages_for(c->len));
+  for (int lp = 0; lp < n_pages && st == CS_OK; lp += cs::kMaxPackPages)
+    st = timed_launch(p, CS_PROF_PACK, "pack launch", [&] {
+      return cs::launch_pack_fp4(p->geom(), slot, c->len, lp, std::min(cs::kMaxPackPages, n_pages - lp), dst, p->stream);
+    });
+  return st;
 }
 
 cs_status cs_kv_pack(const cs_pool* p, cs_conv conv, void* dst, size_t dst_bytes, cs_stream stream) {

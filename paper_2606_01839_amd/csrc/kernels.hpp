@@ -91,8 +91,11 @@ int rope_q_layers(const PoolGeom& g);
 // Read back: chunks (meta: PageChunk[n_chunks]) of the pool to k, v [n_layers][dst_rows][Hkv][D] in bf16.
 hipError_t launch_read(const PoolGeom& g, const Meta& meta, int n_chunks, void* k, void* v, int64_t dst_rows, hipStream_t stream);
 
-// Pack of a conversation (of a pool of either kind) into the wire of a 4-bit pool, and that pool's unpack.
-hipError_t launch_pack_fp4(const PoolGeom& g, int slot, int64_t len, void* wire, hipStream_t stream);
+// Pack of logical pages [lp0, lp0 + n_lp) of a conversation (of a pool of either kind) into the wire of a 4-bit
+// pool, and that pool's unpack. A launch takes at most kMaxPackPages (256 threads a page, and a grid has fewer
+// than 2^32).
+constexpr int kMaxPackPages = (1 << 24) - 1;
+hipError_t launch_pack_fp4(const PoolGeom& g, int slot, int64_t len, int lp0, int n_lp, void* wire, hipStream_t stream);
 hipError_t launch_unpack_fp4(const PoolGeom& g, const void* wire, const Meta& meta, int slot, int64_t len, int lp0, int n_lp,
                              hipStream_t stream);
 

@@ -432,9 +432,9 @@ __device__ __forceinline__ int valid_tokens(int64_t len, int lpage) {
 template <int D>
 __global__ __launch_bounds__(256) void kv_pack_same_fp4_kernel(const uint8_t* __restrict__ pool, int64_t n_pages, int n_kv_heads,
                                                                const int32_t* __restrict__ pt_row, int64_t len,
-                                                               uint8_t* __restrict__ wire, int n_lpages) {
+                                                               uint8_t* __restrict__ wire, int n_lpages, int lp0) {
   using B = Fp4Block<D>;
-  const int lp = blockIdx.x, layer = blockIdx.y;
+  const int lp = lp0 + blockIdx.x, layer = blockIdx.y;
   fp4_copy_page<D>(pool + B::at(layer, pt_row[lp], 0, n_pages, n_kv_heads), wire + B::at(layer, lp, 0, n_lpages, n_kv_heads),
                    n_kv_heads, valid_tokens(len, lp));
 }
@@ -461,13 +461,13 @@ __global__ __launch_bounds__(256) void kv_unpack_fp4_kernel(LaunchMeta, const ui
 template <int D>
 __global__ __launch_bounds__(256) void kv_pack_fp4_kernel(const uint16_t* __restrict__ pool, int64_t n_pages, int n_kv_heads,
                                                           const int32_t* __restrict__ pt_row, int64_t len,
-                                                          uint8_t* __restrict__ wire, int n_lpages) {
+                                                          uint8_t* __restrict__ wire, int n_lpages, int lp0) {
   using B = Fp4Block<D>;
   constexpr int NW = B::kWords;
   const int waves = blockDim.x >> 6, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int c = lane & 15, qd = lane >> 4;
   const int groups = n_kv_heads / waves;
-  const int lp = blockIdx.x, layer = blockIdx.y / groups, head = (blockIdx.y % groups) * waves + wave;
+  const int lp = lp0 + blockIdx.x, layer = blockIdx.y / groups, head = (blockIdx.y % groups) * waves + wave;
   const uint16_t* src = pool + block_elem<D>(layer, pt_row[lp], head, n_pages, n_kv_heads);
   uint8_t* dst = wire + B::at(layer, lp, head, n_lpages, n_kv_heads);
   const int valid = valid_tokens(len, lp);
@@ -630,19 +630,19 @@ hipError_t launch_read(const PoolGeom& g, const Meta& meta, int n_chunks, void* 
   });
 }
 
-hipError_t launch_pack_fp4(const PoolGeom& g, int slot, int64_t len, void* wire, hipStream_t stream) {
+hipError_t launch_pack_fp4(const PoolGeom& g, int slot, int64_t len, int lp0, int n_lp, void* wire, hipStream_t stream) {
+  if (n_lp == 0) return hipSuccess;
   const int n_lpages = static_cast<int>(pages_for(len));
-  if (n_lpages == 0) return hipSuccess;
   const int32_t* pt_row = g.page_table + static_cast<size_t>(slot) * g.max_pages;
   const int waves = head_waves(g.n_kv_heads);
   return by_dim(g.head_dim, [&](auto dc) {
     constexpr int D = decltype(dc)::value;
     if (g.fp4)
-      kv_pack_same_fp4_kernel<D><<<dim3(n_lpages, g.n_layers), 256, 0, stream>>>(
-          static_cast<const uint8_t*>(g.pool), g.n_pages, g.n_kv_heads, pt_row, len, static_cast<uint8_t*>(wire), n_lpages);
+      kv_pack_same_fp4_kernel<D><<<dim3(n_lp, g.n_layers), 256, 0, stream>>>(
+          static_cast<const uint8_t*>(g.pool), g.n_pages, g.n_kv_heads, pt_row, len, static_cast<uint8_t*>(wire), n_lpages, lp0);
     else
-      kv_pack_fp4_kernel<D><<<dim3(n_lpages, g.n_layers * (g.n_kv_heads / waves)), 64 * waves, 0, stream>>>(
-          static_cast<const uint16_t*>(g.pool), g.n_pages, g.n_kv_heads, pt_row, len, static_cast<uint8_t*>(wire), n_lpages);
+      kv_pack_fp4_kernel<D><<<dim3(n_lp, g.n_layers * (g.n_kv_heads / waves)), 64 * waves, 0, stream>>>(
+          static_cast<const uint16_t*>(g.pool), g.n_pages, g.n_kv_heads, pt_row, len, static_cast<uint8_t*>(wire), n_lpages, lp0);
     return hipGetLastError();
   });
 }
