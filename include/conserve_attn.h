@@ -203,7 +203,8 @@ cs_status cs_rope_init(cs_rope* out, int32_t rotary_dim, int32_t interleaved, do
  * call into q_out (same shape; q itself, or no overlap with it), ready for the attention calls.
  * Errors: as cs_kv_append_batch; CS_EINVAL for a null or invalid rope (rotary_dim no multiple of 16 in
  * 16 .. head_dim, interleaved not 0 or 1, amplitude or an inv_freq in use not finite), q without q_out, q of more
- * than 2^28 - 16 rows. After CS_EHIP q_out is undefined: queries rotated in place may or may not have turned.
+ * than 2^28 - 16 rows; CS_ENOMEM for q of more than 2^18 conversations. After CS_EHIP q_out is undefined: queries
+ * rotated in place may or may not have turned.
  */
 cs_status cs_kv_append_rope(cs_pool* pool, const cs_rope* rope, int32_t n_convs, const cs_conv* convs, const int32_t* n_new,
                             const void* k, const void* v, const void* q, void* q_out, cs_stream stream);
@@ -212,7 +213,7 @@ cs_status cs_kv_append_rope(cs_pool* pool, const cs_rope* rope, int32_t n_convs,
  * Queries of the last q_lens[i] positions of each conversation (those the attention calls take), rotated:
  * q, out [n_layers][sum(q_lens)][n_q_heads][head_dim] for any n_layers >= 0; out may be q itself, otherwise
  * they do not overlap. May be captured into a graph, as cs_attn_decode_batch_noalloc. Errors: as cs_attn_extend,
- * and as cs_kv_append_rope for rope and after CS_EHIP; CS_EINVAL (n_layers < 0, more than 2^28 - 16 rows).
+ * and as cs_kv_append_rope for rope, rows, conversations and after CS_EHIP; CS_EINVAL (n_layers < 0).
  */
 cs_status cs_rope_q(cs_pool* pool, const cs_rope* rope, int32_t n_convs, const cs_conv* convs, const int32_t* q_lens,
                     int32_t n_layers, const void* q, void* out, cs_stream stream);

@@ -658,8 +658,6 @@ cs_status check_append(const cs_pool* p, const std::vector<const cs::Conv*>& cv,
   return CS_OK;
 }
 
-// `carry` (may be null): metadata of the launches that follow the append in the same call; on success
-// *carry_dev is its device address.
 struct RotatedAppend {
   cs::RopeArgs rope;
   const void* q = nullptr;   // may be null
@@ -669,15 +667,22 @@ struct RotatedAppend {
 // Rows a query rotation takes at most: 16 a workgroup of 256, and a grid has fewer than 2^32 threads.
 constexpr int64_t kMaxRopeRows = (int64_t(1) << 28) - 16;
 
+// Whether queries of that many rows and conversations can be rotated (their descriptors are one upload).
+cs_status check_rope_q(int64_t rows, size_t n_convs) {
+  if (rows > kMaxRopeRows) return fail(CS_EINVAL, "too many query rows");
+  if (n_convs * sizeof(cs::RopeConv) > kQuarter) return fail(CS_ENOMEM, "batch descriptor exceeds the metadata ring");
+  return CS_OK;
+}
+
 // Queries [n_layers][rows][n_q_heads][head_dim] rotated in launches of their own.
 cs_status run_rope_q(cs_pool* p, const std::vector<cs::RopeConv>& convs, int64_t rows, int32_t n_layers, const cs::RopeArgs& rope,
                      const void* q, void* out) {
-  if (rows > kMaxRopeRows) return fail(CS_EINVAL, "too many query rows");
+  cs_status st = check_rope_q(rows, convs.size());
+  if (st != CS_OK) return st;
   Blob b;
   b.push(convs.data(), convs.size());
-  if (b.bytes.size() > kQuarter) return fail(CS_ENOMEM, "batch descriptor exceeds the metadata ring");
   cs::Meta m;
-  cs_status st = place_meta(p, b, &m);
+  st = place_meta(p, b, &m);
   const cs::PoolGeom g = p->geom();
   const size_t layer_bytes = static_cast<size_t>(rows) * g.n_q_heads * g.head_dim * 2;
   const int per = cs::rope_q_layers(g);   // of one launch
@@ -696,7 +701,9 @@ cs_status run_rope_q(cs_pool* p, const std::vector<cs::RopeConv>& convs, int64_t
 // layers 21.1 against 28.3).
 constexpr int64_t kRopeApartGroups = 512;
 
-// `rotated` (may be null): keys turn on their way into the pages, and the queries with them.
+// `carry` (may be null): metadata of the launches that follow the append in the same call; on success
+// *carry_dev is its device address. `rotated` (may be null): keys turn on their way into the pages, and the
+// queries with them.
 cs_status append_impl(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t* n_new,
                       const void* k, const void* v, cs_stream stream, const Blob* carry = nullptr,
                       void** carry_dev = nullptr, const RotatedAppend* rotated = nullptr) {
@@ -707,6 +714,10 @@ cs_status append_impl(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t
   if (n > 0 && !n_new) return fail(CS_EINVAL, "null n_new");
   int64_t total = 0;
   if ((st = check_append(p, cv, n_new, k, v, &total)) != CS_OK || total == 0) return st;
+  if (rotated && rotated->q) {
+    const auto with_rows = std::count_if(n_new, n_new + n, [](int32_t x) { return x > 0; });
+    if ((st = check_rope_q(total, static_cast<size_t>(with_rows))) != CS_OK) return st;
+  }
   if ((st = ensure_device(p)) != CS_OK) return st;
   if ((st = use_stream(p, as_stream(stream))) != CS_OK) return st;
 
@@ -1283,8 +1294,7 @@ static cs_status mixed_impl(cs_pool* p, const cs_rope* rope, int32_t n_ext, cons
       row += ext_lens[i];
     }
     for (int32_t i = 0; i < n_dec; ++i) rd.push_back({i, static_cast<int32_t>(cv[n_ext + i]->len)});
-    if (std::max(re.size(), rd.size()) * sizeof(cs::RopeConv) > kQuarter)
-      return fail(CS_ENOMEM, "batch descriptor exceeds the metadata ring");
+    if ((st = check_rope_q(ext_rows, re.size())) != CS_OK || (st = check_rope_q(n_dec, rd.size())) != CS_OK) return st;
     if ((st = ensure_device(p)) != CS_OK) return st;
     if ((st = use_stream(p, as_stream(stream))) != CS_OK) return st;
     if (n_ext > 0) st = run_rope_q(p, re, ext_rows, p->desc.n_layers, rotated.rope, q_ext, out_ext);
