@@ -24,10 +24,10 @@
  *    scale is exactly 1/sqrt(head_dim). Query head h reads KV head h / (n_q_heads / n_kv_heads).
  *  - Errors: every call validates all arguments before changing any state; on error it returns a
  *    negative cs_status, changes nothing, and sets a thread-local message (cs_last_error). Nothing
- *    aborts or throws across this ABI. CS_EHIP reports a failing HIP runtime call; an append that
- *    fails so still changes no length and no page (its reserved pages return to the free list);
- *    cs_mixed_step's append is complete when a later attention launch fails; after any CS_EHIP
- *    the outputs of the failing call are undefined.
+ *    aborts or throws across this ABI. CS_EHIP reports a failing HIP runtime call, CS_ENOMEM also host
+ *    memory that ran out; an append that fails so still changes no length and no page (its reserved
+ *    pages return to the free list); cs_mixed_step's append is complete when a later attention launch
+ *    fails; after either the outputs of the failing call are undefined.
  *  - Asynchrony: host metadata (lengths, page tables) is committed when the call returns; kernels
  *    and the small metadata uploads they need are enqueued on `stream` (a hipStream_t, 0 = null
  *    stream). No call synchronises the device, except that switching a pool to another stream
@@ -52,7 +52,7 @@ typedef int32_t cs_status;
 enum {
   CS_OK = 0,
   CS_EINVAL = -1,  /* bad argument: null pointer, bad size, duplicate conversation, wire mismatch */
-  CS_ENOMEM = -2,  /* pool has too few free pages / no free conversation slot / ring too small */
+  CS_ENOMEM = -2,  /* too few free pages / no free conversation slot / ring too small / no host memory */
   CS_ENOENT = -3,  /* unknown or destroyed conversation handle */
   CS_ESTATE = -4,  /* call not valid in the conversation's state (e.g. q_len > length) */
   CS_ERANGE = -5,  /* index out of range (layer, page capacity of a conversation) */

@@ -7,7 +7,6 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
-#include <new>
 #include <string>
 #include <vector>
 
@@ -22,6 +21,18 @@ cs_status fail(cs_status code, const std::string& msg) {
   g_err = msg;
   return code;
 }
+
+// Host memory ran out. Every entry that allocates ends in CS_NO_THROW: no exception leaves a C function.
+cs_status out_of_memory() noexcept {
+  try {
+    g_err = "host allocation failed";
+  } catch (...) {
+    g_err.clear();
+  }
+  return CS_ENOMEM;
+}
+#define CS_NO_THROW \
+  catch (...) { return out_of_memory(); }
 
 constexpr size_t kAlign = 256;
 constexpr size_t kRingBytes = size_t(8) << 20;  // metadata ring (device + pinned host), 4 quarters
@@ -721,8 +732,8 @@ cs_status append_impl(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t
   if ((st = ensure_device(p)) != CS_OK) return st;
   if ((st = use_stream(p, as_stream(stream))) != CS_OK) return st;
 
-  // Reserve pages (cannot fail now) and build the chunks; lengths are committed only after every
-  // upload and launch has been issued. If one of those fails, the reserved pages go back to the
+  // Reserve pages (there are enough) and build the chunks; lengths are committed only after every
+  // upload and launch has been issued. If one of those fails, or host memory runs out, the reserved pages go back to the
   // free list in their old order and nothing about the conversations changes. (Launches already
   // issued may have written the new tokens into the reserved pages and into unused slots past a
   // conversation's end; no kernel reads those: attention masks keys past the length, pack writes
@@ -732,76 +743,79 @@ cs_status append_impl(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t
   std::vector<size_t> old_pages(n);
   std::vector<const std::vector<int32_t>*> lists(n);
   for (int32_t i = 0; i < n; ++i) {
-    cs::Conv* c = p->convs.find(convs[i]);
+    const cs::Conv* c = cv[i];
     slots[i] = cs::ConvTable::slot_of(convs[i]);
     old_lens[i] = c->len;
     old_pages[i] = c->pages.size();
-    p->pages.alloc(cs::pages_for(c->len + n_new[i]) - cs::pages_for(c->len), c->pages);
     lists[i] = &c->pages;
   }
-  std::vector<cs::PageChunk> chunks = cs::plan_append(slots, old_lens, nn, lists);
-  auto roll_back = [&] {
-    std::vector<int32_t> taken;
-    for (int32_t i = 0; i < n; ++i) {
+  auto roll_back = [&] {   // (allocates nothing)
+    for (int32_t i = n - 1; i >= 0; --i) {
       cs::Conv* c = p->convs.find(convs[i]);
-      taken.insert(taken.end(), c->pages.begin() + static_cast<std::ptrdiff_t>(old_pages[i]), c->pages.end());
+      p->pages.unalloc(c->pages, old_pages[i]);
       c->pages.resize(old_pages[i]);
     }
-    p->pages.unalloc(taken);
   };
 
-  const cs::PoolGeom g = p->geom();
-  const size_t carry_bytes = carry ? carry->bytes.size() : 0;
-  const bool q_apart = rotated && rotated->q && cs::append_rope_groups(g, chunks.size()) > kRopeApartGroups;
-  auto launch = [&](const cs::Meta& m, int n_chunks, const cs::AppendCarry& c) {
-    return timed_launch(p, CS_PROF_APPEND, "append launch", [&] {
-      if (rotated)
-        return cs::launch_append_as(g, m, n_chunks, c, &rotated->rope, k, v, q_apart ? nullptr : rotated->q, rotated->q_out, total,
-                                    p->stream);
-      if (p->fp4) return cs::launch_append_as(g, m, n_chunks, c, nullptr, k, v, nullptr, nullptr, total, p->stream);
-      return cs::launch_append(g, m, n_chunks, c, k, v, total, p->stream);
-    });
-  };
-  if (chunks.size() * sizeof(cs::PageChunk) + carry_bytes <= cs::kMetaBytes) {
-    // small: the chunks travel in the launch's arguments, and so does the metadata of the launches
-    // that follow, which the append kernel stores to the ring's device half.
-    Blob b;
-    b.push(chunks.data(), chunks.size());
-    cs::AppendCarry c;
-    if (carry_bytes > 0) {
-      size_t off = 0;
-      bool captured = false;   // (the append kernel stores it either way)
-      st = ring_reserve(p, carry_bytes, &off, &captured);
-      c.dst = p->ws + p->lay.ring + off;
-      c.bytes = carry_bytes;
-      c.off = b.push(carry->bytes.data(), carry_bytes);
-      *carry_dev = c.dst;
+  try {
+    for (int32_t i = 0; i < n; ++i)
+      p->pages.alloc(cs::pages_for(old_lens[i] + n_new[i]) - cs::pages_for(old_lens[i]), p->convs.find(convs[i])->pages);
+    const std::vector<cs::PageChunk> chunks = cs::plan_append(slots, old_lens, nn, lists);
+    const cs::PoolGeom g = p->geom();
+    const size_t carry_bytes = carry ? carry->bytes.size() : 0;
+    const bool q_apart = rotated && rotated->q && cs::append_rope_groups(g, chunks.size()) > kRopeApartGroups;
+    auto launch = [&](const cs::Meta& m, int n_chunks, const cs::AppendCarry& c) {
+      return timed_launch(p, CS_PROF_APPEND, "append launch", [&] {
+        if (rotated)
+          return cs::launch_append_as(g, m, n_chunks, c, &rotated->rope, k, v, q_apart ? nullptr : rotated->q, rotated->q_out, total,
+                                      p->stream);
+        if (p->fp4) return cs::launch_append_as(g, m, n_chunks, c, nullptr, k, v, nullptr, nullptr, total, p->stream);
+        return cs::launch_append(g, m, n_chunks, c, k, v, total, p->stream);
+      });
+    };
+    if (chunks.size() * sizeof(cs::PageChunk) + carry_bytes <= cs::kMetaBytes) {
+      // small: the chunks travel in the launch's arguments, and so does the metadata of the launches
+      // that follow, which the append kernel stores to the ring's device half.
+      Blob b;
+      b.push(chunks.data(), chunks.size());
+      cs::AppendCarry c;
+      if (carry_bytes > 0) {
+        size_t off = 0;
+        bool captured = false;   // (the append kernel stores it either way)
+        st = ring_reserve(p, carry_bytes, &off, &captured);
+        c.dst = p->ws + p->lay.ring + off;
+        c.bytes = carry_bytes;
+        c.off = b.push(carry->bytes.data(), carry_bytes);
+        *carry_dev = c.dst;
+      }
+      cs::Meta m;
+      m.host = b.bytes.data();
+      m.bytes = b.bytes.size();
+      if (st == CS_OK) st = launch(m, static_cast<int>(chunks.size()), c);
+    } else {
+      const size_t per = kQuarter / sizeof(cs::PageChunk) - 1;
+      for (size_t c0 = 0; c0 < chunks.size() && st == CS_OK; c0 += per) {
+        const size_t c1 = std::min(chunks.size(), c0 + per);
+        void* d = nullptr;
+        st = upload(p, chunks.data() + c0, (c1 - c0) * sizeof(cs::PageChunk), &d);
+        if (st == CS_OK)
+          st = launch(meta_part(d, 0, (c1 - c0) * sizeof(cs::PageChunk)), static_cast<int>(c1 - c0), {});
+      }
+      // After the chunks, which may go round the ring: nothing of it is reused before the launches that read
+      // the carried metadata are issued.
+      if (carry_bytes > 0 && st == CS_OK) st = upload(p, carry->bytes.data(), carry_bytes, carry_dev);
     }
-    cs::Meta m;
-    m.host = b.bytes.data();
-    m.bytes = b.bytes.size();
-    if (st == CS_OK) st = launch(m, static_cast<int>(chunks.size()), c);
-  } else {
-    const size_t per = kQuarter / sizeof(cs::PageChunk) - 1;
-    for (size_t c0 = 0; c0 < chunks.size() && st == CS_OK; c0 += per) {
-      const size_t c1 = std::min(chunks.size(), c0 + per);
-      void* d = nullptr;
-      st = upload(p, chunks.data() + c0, (c1 - c0) * sizeof(cs::PageChunk), &d);
-      if (st == CS_OK)
-        st = launch(meta_part(d, 0, (c1 - c0) * sizeof(cs::PageChunk)), static_cast<int>(c1 - c0), {});
+    if (q_apart && st == CS_OK) {
+      std::vector<cs::RopeConv> rc;
+      int32_t row = 0;
+      for (int32_t i = 0; i < n; ++i) {
+        if (nn[i] > 0) rc.push_back({row, static_cast<int32_t>(old_lens[i])});
+        row += nn[i];
+      }
+      st = run_rope_q(p, rc, total, g.n_layers, rotated->rope, rotated->q, rotated->q_out);
     }
-    // After the chunks, which may go round the ring: nothing of it is reused before the launches that read
-    // the carried metadata are issued.
-    if (carry_bytes > 0 && st == CS_OK) st = upload(p, carry->bytes.data(), carry_bytes, carry_dev);
-  }
-  if (q_apart && st == CS_OK) {
-    std::vector<cs::RopeConv> rc;
-    int32_t row = 0;
-    for (int32_t i = 0; i < n; ++i) {
-      if (nn[i] > 0) rc.push_back({row, static_cast<int32_t>(old_lens[i])});
-      row += nn[i];
-    }
-    st = run_rope_q(p, rc, total, g.n_layers, rotated->rope, rotated->q, rotated->q_out);
+  } catch (...) {
+    st = out_of_memory();
   }
   if (st != CS_OK) {
     roll_back();
@@ -831,12 +845,12 @@ size_t cs_pool_workspace_bytes(const cs_pool_desc* d) {
 }
 
 cs_status cs_pool_create(const cs_pool_desc* d, void* kv_base, size_t kv_bytes, void* ws_base,
-                         size_t ws_bytes, uint64_t seed, cs_pool** out) {
+                         size_t ws_bytes, uint64_t seed, cs_pool** out) try {
   return cs_pool_create_as(d, CS_KV_BF16, kv_base, kv_bytes, ws_base, ws_bytes, seed, out);
-}
+} CS_NO_THROW
 
 cs_status cs_pool_create_as(const cs_pool_desc* d, int32_t format, void* kv_base, size_t kv_bytes, void* ws_base,
-                            size_t ws_bytes, uint64_t seed, cs_pool** out) {
+                            size_t ws_bytes, uint64_t seed, cs_pool** out) try {
   if (const char* why = desc_problem(d)) return fail(CS_EINVAL, why);
   if (format != CS_KV_BF16 && format != CS_KV_FP4) return fail(CS_EINVAL, "unknown KV format");
   if (!out) return fail(CS_EINVAL, "null out");
@@ -846,14 +860,11 @@ cs_status cs_pool_create_as(const cs_pool_desc* d, int32_t format, void* kv_base
   if (kv_bytes < cs_pool_kv_bytes_as(d, format)) return fail(CS_EINVAL, "kv buffer smaller than cs_pool_kv_bytes");
   if (ws_bytes < cs_pool_workspace_bytes(d))
     return fail(CS_EINVAL, "workspace smaller than cs_pool_workspace_bytes");
-  cs_pool* p = new (std::nothrow)
-      cs_pool(*d, format == CS_KV_FP4, static_cast<char*>(kv_base), kv_bytes, static_cast<char*>(ws_base), ws_bytes, seed);
-  if (!p) return fail(CS_ENOMEM, "host allocation failed");
-  *out = p;
+  *out = new cs_pool(*d, format == CS_KV_FP4, static_cast<char*>(kv_base), kv_bytes, static_cast<char*>(ws_base), ws_bytes, seed);
   return CS_OK;
-}
+} CS_NO_THROW
 
-cs_status cs_pool_destroy(cs_pool* p) {
+cs_status cs_pool_destroy(cs_pool* p) try {
   if (!p) return fail(CS_EINVAL, "null pool");
   cs_status st = CS_OK;
   if (p->dev_ready) {
@@ -877,37 +888,37 @@ cs_status cs_pool_destroy(cs_pool* p) {
   }
   delete p;
   return st;
-}
+} CS_NO_THROW
 
-cs_status cs_pool_occupancy(const cs_pool* p, int64_t* used, int64_t* free_pages) {
+cs_status cs_pool_occupancy(const cs_pool* p, int64_t* used, int64_t* free_pages) try {
   if (!p || !used || !free_pages) return fail(CS_EINVAL, "null argument");
   *used = p->pages.used_count();
   *free_pages = p->pages.free_count();
   return CS_OK;
-}
+} CS_NO_THROW
 
-cs_status cs_conv_create(cs_pool* p, cs_conv* out) {
+cs_status cs_conv_create(cs_pool* p, cs_conv* out) try {
   if (!p || !out) return fail(CS_EINVAL, "null argument");
   if (!p->convs.create(out)) return fail(CS_ENOMEM, "all conversation slots are live");
   return CS_OK;
-}
+} CS_NO_THROW
 
-cs_status cs_conv_destroy(cs_pool* p, cs_conv conv) {
+cs_status cs_conv_destroy(cs_pool* p, cs_conv conv) try {
   if (!p) return fail(CS_EINVAL, "null pool");
   if (!p->convs.find(conv)) return fail(CS_ENOENT, "unknown conversation handle");
   p->convs.destroy(conv, p->pages);
   return CS_OK;
-}
+} CS_NO_THROW
 
-cs_status cs_conv_len(const cs_pool* p, cs_conv conv, int64_t* tokens) {
+cs_status cs_conv_len(const cs_pool* p, cs_conv conv, int64_t* tokens) try {
   if (!p || !tokens) return fail(CS_EINVAL, "null argument");
   const cs::Conv* c = p->convs.find(conv);
   if (!c) return fail(CS_ENOENT, "unknown conversation handle");
   *tokens = c->len;
   return CS_OK;
-}
+} CS_NO_THROW
 
-cs_status cs_conv_pages(const cs_pool* p, cs_conv conv, int32_t* out, int64_t cap, int64_t* n) {
+cs_status cs_conv_pages(const cs_pool* p, cs_conv conv, int32_t* out, int64_t cap, int64_t* n) try {
   if (!p || !n) return fail(CS_EINVAL, "null argument");
   const cs::Conv* c = p->convs.find(conv);
   if (!c) return fail(CS_ENOENT, "unknown conversation handle");
@@ -916,20 +927,20 @@ cs_status cs_conv_pages(const cs_pool* p, cs_conv conv, int32_t* out, int64_t ca
   if (*n > 0 && !out) return fail(CS_EINVAL, "null output");
   std::copy(c->pages.begin(), c->pages.end(), out);
   return CS_OK;
-}
+} CS_NO_THROW
 
 cs_status cs_kv_append(cs_pool* p, cs_conv conv, int32_t n_new, const void* k, const void* v,
-                       cs_stream stream) {
+                       cs_stream stream) try {
   return append_impl(p, 1, &conv, &n_new, k, v, stream);
-}
+} CS_NO_THROW
 
 cs_status cs_kv_append_batch(cs_pool* p, int32_t n_convs, const cs_conv* convs, const int32_t* n_new,
-                             const void* k, const void* v, cs_stream stream) {
+                             const void* k, const void* v, cs_stream stream) try {
   return append_impl(p, n_convs, convs, n_new, k, v, stream);
-}
+} CS_NO_THROW
 
 cs_status cs_rope_init(cs_rope* out, int32_t rotary_dim, int32_t interleaved, double base, int32_t scaling, double factor,
-                       double original_len, double low_turns, double high_turns) {
+                       double original_len, double low_turns, double high_turns) try {
   if (!out) return fail(CS_EINVAL, "null out");
   if (rotary_dim < 16 || rotary_dim > 128 || rotary_dim % 16) return fail(CS_EINVAL, "rotary_dim must be a multiple of 16 in 16 .. 128");
   if (interleaved != 0 && interleaved != 1) return fail(CS_EINVAL, "interleaved must be 0 or 1");
@@ -956,10 +967,10 @@ cs_status cs_rope_init(cs_rope* out, int32_t rotary_dim, int32_t interleaved, do
   }
   *out = r;
   return CS_OK;
-}
+} CS_NO_THROW
 
 cs_status cs_kv_append_rope(cs_pool* p, const cs_rope* rope, int32_t n_convs, const cs_conv* convs, const int32_t* n_new,
-                            const void* k, const void* v, const void* q, void* q_out, cs_stream stream) {
+                            const void* k, const void* v, const void* q, void* q_out, cs_stream stream) try {
   if (!p) return fail(CS_EINVAL, "null pool");
   RotatedAppend r;
   const cs_status st = rope_args(p->desc, rope, &r.rope);
@@ -968,10 +979,10 @@ cs_status cs_kv_append_rope(cs_pool* p, const cs_rope* rope, int32_t n_convs, co
   r.q = q;
   r.q_out = q_out;
   return append_impl(p, n_convs, convs, n_new, k, v, stream, nullptr, nullptr, &r);
-}
+} CS_NO_THROW
 
 cs_status cs_rope_q(cs_pool* p, const cs_rope* rope, int32_t n, const cs_conv* convs, const int32_t* q_lens, int32_t n_layers,
-                    const void* q, void* out, cs_stream stream) {
+                    const void* q, void* out, cs_stream stream) try {
   if (!p) return fail(CS_EINVAL, "null pool");
   cs::RopeArgs r;
   cs_status st = rope_args(p->desc, rope, &r);
@@ -996,10 +1007,10 @@ cs_status cs_rope_q(cs_pool* p, const cs_rope* rope, int32_t n, const cs_conv* c
   if ((st = ensure_device(p)) != CS_OK) return st;
   if ((st = use_stream(p, as_stream(stream))) != CS_OK) return st;
   return run_rope_q(p, rc, rows, n_layers, r, q, out);
-}
+} CS_NO_THROW
 
 cs_status cs_kv_read(cs_pool* p, int32_t n, const cs_conv* convs, const int64_t* starts, const int32_t* counts, void* k, void* v,
-                     cs_stream stream) {
+                     cs_stream stream) try {
   if (!p) return fail(CS_EINVAL, "null pool");
   std::vector<const cs::Conv*> cv;
   cs_status st = check_convs(p, n, convs, cv);
@@ -1037,20 +1048,20 @@ cs_status cs_kv_read(cs_pool* p, int32_t n, const cs_conv* convs, const int64_t*
       });
   }
   return st;
-}
+} CS_NO_THROW
 
 cs_status cs_attn_prefill_turn1(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t* q_lens,
-                                int32_t layer, const void* q, void* out, cs_stream stream) {
+                                int32_t layer, const void* q, void* out, cs_stream stream) try {
   return attend(p, n, convs, q_lens, layer, q, out, stream, true);
-}
+} CS_NO_THROW
 
 cs_status cs_attn_extend(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t* q_lens,
-                         int32_t layer, const void* q, void* out, cs_stream stream) {
+                         int32_t layer, const void* q, void* out, cs_stream stream) try {
   return attend(p, n, convs, q_lens, layer, q, out, stream, false);
-}
+} CS_NO_THROW
 
 cs_status cs_attn_decode_batch(cs_pool* p, int32_t n, const cs_conv* convs, int32_t layer,
-                               const void* q, void* out, cs_stream stream) {
+                               const void* q, void* out, cs_stream stream) try {
   if (!p) return fail(CS_EINVAL, "null pool");
   std::vector<const cs::Conv*> cv;
   cs_status st = check_convs(p, n, convs, cv);
@@ -1073,10 +1084,10 @@ cs_status cs_attn_decode_batch(cs_pool* p, int32_t n, const cs_conv* convs, int3
   DecodeWork w;
   if ((st = place_decode(p, plan, &w)) != CS_OK) return st;
   return launch_decode_layers(p, w, layer, 1, q, out);
-}
+} CS_NO_THROW
 
 cs_status cs_attn_decode_batch_noalloc(cs_pool* p, int32_t n, const cs_conv* convs, int32_t layer,
-                                       const void* q, void* out, cs_stream stream) {
+                                       const void* q, void* out, cs_stream stream) try {
   if (!p) return fail(CS_EINVAL, "null pool");
   std::vector<const cs::Conv*> cv;
   cs_status st = check_convs(p, n, convs, cv);
@@ -1117,23 +1128,23 @@ cs_status cs_attn_decode_batch_noalloc(cs_pool* p, int32_t n, const cs_conv* con
   if (w.single) return CS_OK;
   CS_HIP(cs::launch_decode_merge(g, 1, w.w, scratch, out, p->stream), "decode merge launch");
   return CS_OK;
-}
+} CS_NO_THROW
 
-cs_status cs_kv_pack_size(const cs_pool* p, cs_conv conv, size_t* bytes) {
+cs_status cs_kv_pack_size(const cs_pool* p, cs_conv conv, size_t* bytes) try {
   if (!p || !bytes) return fail(CS_EINVAL, "null argument");
   const cs::Conv* c = p->convs.find(conv);
   if (!c) return fail(CS_ENOENT, "unknown conversation handle");
   *bytes = wire_size(p->desc, p->fp4, c->len);
   return CS_OK;
-}
+} CS_NO_THROW
 
-cs_status cs_kv_pack_fp4_size(const cs_pool* p, cs_conv conv, size_t* bytes) {
+cs_status cs_kv_pack_fp4_size(const cs_pool* p, cs_conv conv, size_t* bytes) try {
   if (!p || !bytes) return fail(CS_EINVAL, "null argument");
   const cs::Conv* c = p->convs.find(conv);
   if (!c) return fail(CS_ENOENT, "unknown conversation handle");
   *bytes = wire_size(p->desc, true, c->len);
   return CS_OK;
-}
+} CS_NO_THROW
 
 static cs_status pack_impl(const cs_pool* pc, cs_conv conv, bool fp4, void* dst, size_t dst_bytes, cs_stream stream) {
   cs_pool* p = const_cast<cs_pool*>(pc);  // host metadata is unchanged; stream/ring state is not
@@ -1158,16 +1169,16 @@ static cs_status pack_impl(const cs_pool* pc, cs_conv conv, bool fp4, void* dst,
   return st;
 }
 
-cs_status cs_kv_pack(const cs_pool* p, cs_conv conv, void* dst, size_t dst_bytes, cs_stream stream) {
+cs_status cs_kv_pack(const cs_pool* p, cs_conv conv, void* dst, size_t dst_bytes, cs_stream stream) try {
   return pack_impl(p, conv, p && p->fp4, dst, dst_bytes, stream);
-}
+} CS_NO_THROW
 
-cs_status cs_kv_pack_fp4(const cs_pool* p, cs_conv conv, void* dst, size_t dst_bytes, cs_stream stream) {
+cs_status cs_kv_pack_fp4(const cs_pool* p, cs_conv conv, void* dst, size_t dst_bytes, cs_stream stream) try {
   return pack_impl(p, conv, true, dst, dst_bytes, stream);
-}
+} CS_NO_THROW
 
 cs_status cs_kv_unpack(cs_pool* p, const void* src, size_t src_bytes, int64_t n_tokens,
-                       cs_conv* out_conv, cs_stream stream) {
+                       cs_conv* out_conv, cs_stream stream) try {
   if (!p || !out_conv) return fail(CS_EINVAL, "null argument");
   if (n_tokens < 1) return fail(CS_EINVAL, "n_tokens must be >= 1");
   if (!src) return fail(CS_EINVAL, "null src");
@@ -1180,10 +1191,13 @@ cs_status cs_kv_unpack(cs_pool* p, const void* src, size_t src_bytes, int64_t n_
   cs_status st;
   if ((st = ensure_device(p)) != CS_OK) return st;
   if ((st = use_stream(p, as_stream(stream))) != CS_OK) return st;
+  std::vector<int32_t> pages;
+  pages.reserve(static_cast<size_t>(np));   // (before anything changes)
+  p->pages.alloc(np, pages);
   cs_conv h;
   p->convs.create(&h);
   cs::Conv* c = p->convs.find(h);
-  p->pages.alloc(np, c->pages);
+  c->pages.swap(pages);
   c->len = n_tokens;
   *out_conv = h;
   const size_t per = kQuarter / sizeof(int32_t) - 64;
@@ -1203,7 +1217,7 @@ cs_status cs_kv_unpack(cs_pool* p, const void* src, size_t src_bytes, int64_t n_
     if (st != CS_OK) return st;
   }
   return CS_OK;
-}
+} CS_NO_THROW
 
 // `rope` (may be null): the new tokens' keys and queries turn by their positions.
 static cs_status mixed_impl(cs_pool* p, const cs_rope* rope, int32_t n_ext, const cs_conv* ext_convs, const int32_t* ext_lens,
@@ -1410,18 +1424,18 @@ static cs_status mixed_impl(cs_pool* p, const cs_rope* rope, int32_t n_ext, cons
 cs_status cs_mixed_step(cs_pool* p, int32_t n_ext, const cs_conv* ext_convs, const int32_t* ext_lens,
                         int32_t n_dec, const cs_conv* dec_convs, const void* k, const void* v,
                         const void* q_ext, void* out_ext, const void* q_dec, void* out_dec,
-                        uint32_t flags, cs_stream stream) {
+                        uint32_t flags, cs_stream stream) try {
   return mixed_impl(p, nullptr, n_ext, ext_convs, ext_lens, n_dec, dec_convs, k, v, q_ext, out_ext, q_dec, out_dec, flags, stream);
-}
+} CS_NO_THROW
 
 cs_status cs_mixed_step_rope(cs_pool* p, const cs_rope* rope, int32_t n_ext, const cs_conv* ext_convs, const int32_t* ext_lens,
                              int32_t n_dec, const cs_conv* dec_convs, const void* k, const void* v, const void* q_ext,
-                             void* out_ext, const void* q_dec, void* out_dec, uint32_t flags, cs_stream stream) {
+                             void* out_ext, const void* q_dec, void* out_dec, uint32_t flags, cs_stream stream) try {
   if (!rope) return fail(CS_EINVAL, "null rope");
   return mixed_impl(p, rope, n_ext, ext_convs, ext_lens, n_dec, dec_convs, k, v, q_ext, out_ext, q_dec, out_dec, flags, stream);
-}
+} CS_NO_THROW
 
-cs_status cs_device_info(int32_t device, cs_device_info_t* out) {
+cs_status cs_device_info(int32_t device, cs_device_info_t* out) try {
   if (!out) return fail(CS_EINVAL, "null out");
   hipDeviceProp_t pr;
   CS_HIP(hipGetDeviceProperties(&pr, device), "hipGetDeviceProperties");
@@ -1437,9 +1451,9 @@ cs_status cs_device_info(int32_t device, cs_device_info_t* out) {
   out->l2_bytes = pr.l2CacheSize;
   out->total_mem_bytes = static_cast<int64_t>(pr.totalGlobalMem);
   return CS_OK;
-}
+} CS_NO_THROW
 
-cs_status cs_probe_stream_read(const void* src, size_t bytes, void* sink, cs_stream stream) {
+cs_status cs_probe_stream_read(const void* src, size_t bytes, void* sink, cs_stream stream) try {
   if (!src || !sink) return fail(CS_EINVAL, "null src or sink");
   if (bytes % 16) return fail(CS_EINVAL, "bytes must be a multiple of 16");
   int dev = 0, cus = 0;
@@ -1448,15 +1462,15 @@ cs_status cs_probe_stream_read(const void* src, size_t bytes, void* sink, cs_str
   CS_HIP(cs::launch_stream_read_probe(src, bytes, static_cast<uint32_t*>(sink), cus, as_stream(stream)),
          "stream read probe launch");
   return CS_OK;
-}
+} CS_NO_THROW
 
-cs_status cs_debug_fail_launches(cs_pool* p, int64_t after) {
+cs_status cs_debug_fail_launches(cs_pool* p, int64_t after) try {
   if (!p) return fail(CS_EINVAL, "null pool");
   p->fail_after = after < 0 ? -1 : after;
   return CS_OK;
-}
+} CS_NO_THROW
 
-cs_status cs_profile_start(cs_pool* p) {
+cs_status cs_profile_start(cs_pool* p) try {
   if (!p) return fail(CS_EINVAL, "null pool");
   for (auto& pe : p->prof_events) {
     p->ev_free.push_back(pe.start);
@@ -1465,9 +1479,9 @@ cs_status cs_profile_start(cs_pool* p) {
   p->prof_events.clear();
   p->prof_on = true;
   return CS_OK;
-}
+} CS_NO_THROW
 
-cs_status cs_profile_stop(cs_pool* p, double* ms, int64_t* launches) {
+cs_status cs_profile_stop(cs_pool* p, double* ms, int64_t* launches) try {
   if (!p || !ms || !launches) return fail(CS_EINVAL, "null argument");
   for (int k = 0; k < CS_PROF_KINDS; ++k) {
     ms[k] = 0.0;
@@ -1485,10 +1499,11 @@ cs_status cs_profile_stop(cs_pool* p, double* ms, int64_t* launches) {
   }
   p->prof_events.clear();
   return CS_OK;
-}
+} CS_NO_THROW
 
 }  // extern "C"
 namespace cs {
 // Error reporting shared with the other C-ABI translation units (sched_capi.cpp).
 cs_status api_fail(cs_status code, const char* msg) { return fail(code, msg); }
+cs_status api_out_of_memory() noexcept { return out_of_memory(); }
 }  // namespace cs

@@ -35,8 +35,8 @@ void PagePool::release(const std::vector<int32_t>& pages) {
   }
 }
 
-void PagePool::unalloc(const std::vector<int32_t>& pages) {
-  for (auto it = pages.rbegin(); it != pages.rend(); ++it) free_.push_back(*it);
+void PagePool::unalloc(const std::vector<int32_t>& pages, size_t keep) {
+  for (size_t i = pages.size(); i > keep; --i) free_.push_back(pages[i - 1]);
 }
 
 ConvTable::ConvTable(int32_t max_convs, int32_t max_pages_per_conv)
@@ -74,6 +74,7 @@ const Conv* ConvTable::find(int32_t handle) const {
 void ConvTable::destroy(int32_t handle, PagePool& pool) {
   int32_t s = slot_of(handle);
   Conv& c = slots_[static_cast<size_t>(s)];
+  free_slots_.push_back(s);   // (may throw: before anything changes)
   pool.release(c.pages);
   c.pages.clear();
   c.pages.shrink_to_fit();
@@ -81,7 +82,6 @@ void ConvTable::destroy(int32_t handle, PagePool& pool) {
   c.live = false;
   c.gen = (c.gen + 1) & 0x7FFu;
   --live_;
-  free_slots_.push_back(s);
 }
 
 // The items and launch order of a plan with splits of `split` keys.

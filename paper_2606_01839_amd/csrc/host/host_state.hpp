@@ -38,9 +38,9 @@ class PagePool {
   // All-or-nothing: appends n page ids to `out` and returns true, or changes nothing.
   bool alloc(int64_t n, std::vector<int32_t>& out);
   void release(const std::vector<int32_t>& pages);
-  // Undo the latest alloc calls exactly: `pages` are the ids they handed out, in order (the free
-  // list then holds the same ids in the same order as before them).
-  void unalloc(const std::vector<int32_t>& pages);
+  // Undo the latest alloc calls exactly: `pages` from index `keep` on are the ids they handed out, in order
+  // (the free list then holds the same ids in the same order as before them). Allocates nothing.
+  void unalloc(const std::vector<int32_t>& pages, size_t keep = 0);
 
  private:
   int64_t n_pages_;

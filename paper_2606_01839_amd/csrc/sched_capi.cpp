@@ -3,7 +3,7 @@
 #include "conserve_sched.h"
 
 #include <cmath>
-#include <new>
+#include <memory>
 #include <vector>
 
 #include "host/host_state.hpp"
@@ -11,7 +11,10 @@
 
 namespace cs {
 cs_status api_fail(cs_status code, const char* msg);  // capi.cpp: sets cs_last_error()
+cs_status api_out_of_memory() noexcept;
 }  // namespace cs
+#define CS_NO_THROW \
+  catch (...) { return cs::api_out_of_memory(); }   // as in capi.cpp
 
 struct cs_sched {
   cs::Admission admission;
@@ -22,7 +25,7 @@ struct cs_sched {
 extern "C" {
 
 cs_status cs_prefill_curve_fit(int32_t n, const int64_t* tokens, const double* seconds,
-                               cs_prefill_curve* out, double* r2) {
+                               cs_prefill_curve* out, double* r2) try {
   if (!tokens || !seconds || !out) return cs::api_fail(CS_EINVAL, "null argument");
   cs::PrefillCurve c;
   if (!cs::fit_prefill_curve(tokens, seconds, n, &c, r2))
@@ -31,9 +34,9 @@ cs_status cs_prefill_curve_fit(int32_t n, const int64_t* tokens, const double* s
   out->c1 = c.c1;
   out->c2 = c.c2;
   return CS_OK;
-}
+} CS_NO_THROW
 
-cs_status cs_prefill_curve_eval(const cs_prefill_curve* curve, int64_t tokens, double* seconds) {
+cs_status cs_prefill_curve_eval(const cs_prefill_curve* curve, int64_t tokens, double* seconds) try {
   if (!curve || !seconds) return cs::api_fail(CS_EINVAL, "null argument");
   cs::PrefillCurve c;
   c.c0 = curve->c0;
@@ -41,13 +44,13 @@ cs_status cs_prefill_curve_eval(const cs_prefill_curve* curve, int64_t tokens, d
   c.c2 = curve->c2;
   *seconds = c.eval(tokens);
   return CS_OK;
-}
+} CS_NO_THROW
 
 cs_status cs_provision_decoders(double prefill_tokens_per_s, double mean_turn1_tokens,
                                 double decoder_tokens_per_s, double mean_decoder_tokens,
                                 double convs_per_decoder, double mean_lifetime_s,
                                 double* saturation_rate, double* n_throughput, double* n_memory,
-                                int32_t* n_decoders) {
+                                int32_t* n_decoders) try {
   cs::Provisioning p;
   if (!cs::provision_decoders(prefill_tokens_per_s, mean_turn1_tokens, decoder_tokens_per_s,
                               mean_decoder_tokens, convs_per_decoder, mean_lifetime_s, &p))
@@ -57,10 +60,10 @@ cs_status cs_provision_decoders(double prefill_tokens_per_s, double mean_turn1_t
   if (n_memory) *n_memory = p.n_memory;
   if (n_decoders) *n_decoders = p.n_decoders;
   return CS_OK;
-}
+} CS_NO_THROW
 
 cs_status cs_place_least_occupied(int32_t n, const int64_t* used_pages, const int64_t* free_pages,
-                                  int64_t need_pages, int32_t* decoder) {
+                                  int64_t need_pages, int32_t* decoder) try {
   if (!used_pages || !free_pages || !decoder || n < 1)
     return cs::api_fail(CS_EINVAL, "null argument or n < 1");
   if (need_pages < 0) return cs::api_fail(CS_EINVAL, "need_pages < 0");
@@ -70,10 +73,10 @@ cs_status cs_place_least_occupied(int32_t n, const int64_t* used_pages, const in
   *decoder = d;
   if (d < 0) return cs::api_fail(CS_ENOMEM, "no decoder has enough free pages");
   return CS_OK;
-}
+} CS_NO_THROW
 
 cs_status cs_sched_create(const cs_prefill_curve* curve, double max_wait_s, int32_t n_decoders,
-                          cs_pool* const* decoders, cs_sched** out) {
+                          cs_pool* const* decoders, cs_sched** out) try {
   if (!curve || !out) return cs::api_fail(CS_EINVAL, "null argument");
   if (n_decoders < 0) return cs::api_fail(CS_EINVAL, "n_decoders < 0");
   if (n_decoders > 0 && !decoders) return cs::api_fail(CS_EINVAL, "null decoder array");
@@ -85,30 +88,29 @@ cs_status cs_sched_create(const cs_prefill_curve* curve, double max_wait_s, int3
   c.c0 = curve->c0;
   c.c1 = curve->c1;
   c.c2 = curve->c2;
-  cs_sched* s = new (std::nothrow) cs_sched(c, max_wait_s);
-  if (!s) return cs::api_fail(CS_ENOMEM, "out of host memory");
+  auto s = std::make_unique<cs_sched>(c, max_wait_s);
   if (n_decoders > 0) s->decoders.assign(decoders, decoders + n_decoders);
-  *out = s;
+  *out = s.release();
   return CS_OK;
-}
+} CS_NO_THROW
 
-cs_status cs_sched_destroy(cs_sched* sched) {
+cs_status cs_sched_destroy(cs_sched* sched) try {
   if (!sched) return cs::api_fail(CS_EINVAL, "null scheduler");
   delete sched;
   return CS_OK;
-}
+} CS_NO_THROW
 
 cs_status cs_sched_admit(cs_sched* sched, int64_t turn1_tokens, double now_s, double* start_s,
-                         double* done_s) {
+                         double* done_s) try {
   if (!sched) return cs::api_fail(CS_EINVAL, "null scheduler");
   if (turn1_tokens < 1) return cs::api_fail(CS_EINVAL, "turn1_tokens < 1");
   if (!std::isfinite(now_s)) return cs::api_fail(CS_EINVAL, "now_s not finite");
   if (!sched->admission.admit(turn1_tokens, now_s, start_s, done_s))
     return cs::api_fail(CS_EBUSY, "prefiller saturated: expected wait exceeds max_wait_s");
   return CS_OK;
-}
+} CS_NO_THROW
 
-cs_status cs_sched_bind(cs_sched* sched, int64_t kv_tokens, int32_t* decoder) {
+cs_status cs_sched_bind(cs_sched* sched, int64_t kv_tokens, int32_t* decoder) try {
   if (!sched || !decoder) return cs::api_fail(CS_EINVAL, "null argument");
   if (kv_tokens < 1) return cs::api_fail(CS_EINVAL, "kv_tokens < 1");
   const int32_t n = static_cast<int32_t>(sched->decoders.size());
@@ -122,6 +124,6 @@ cs_status cs_sched_bind(cs_sched* sched, int64_t kv_tokens, int32_t* decoder) {
   *decoder = d;
   if (d < 0) return cs::api_fail(CS_ENOMEM, "no decoder has enough free pages");
   return CS_OK;
-}
+} CS_NO_THROW
 
 }  // extern "C"
