@@ -1199,23 +1199,32 @@ cs_status cs_kv_unpack(cs_pool* p, const void* src, size_t src_bytes, int64_t n_
   cs::Conv* c = p->convs.find(h);
   c->pages.swap(pages);
   c->len = n_tokens;
-  *out_conv = h;
-  const size_t per = kQuarter / sizeof(int32_t) - 64;
-  for (size_t p0 = 0; p0 < c->pages.size(); p0 += per) {
-    const size_t p1 = std::min(c->pages.size(), p0 + per);
-    Blob b;
-    b.push(c->pages.data() + p0, p1 - p0);
-    cs::Meta m;
-    if ((st = place_meta(p, b, &m)) != CS_OK) return st;
-    st = timed_launch(p, CS_PROF_UNPACK, "unpack launch", [&] {
-      if (p->fp4)
-        return cs::launch_unpack_fp4(p->geom(), src, m, cs::ConvTable::slot_of(h), n_tokens, static_cast<int>(p0),
-                                     static_cast<int>(p1 - p0), p->stream);
-      return cs::launch_unpack(p->geom(), src, m, cs::ConvTable::slot_of(h),
-                               n_tokens, static_cast<int>(p0), static_cast<int>(p1 - p0), p->stream);
-    });
-    if (st != CS_OK) return st;
+  try {
+    const size_t per = kQuarter / sizeof(int32_t) - 64;
+    for (size_t p0 = 0; p0 < c->pages.size() && st == CS_OK; p0 += per) {
+      const size_t p1 = std::min(c->pages.size(), p0 + per);
+      Blob b;
+      b.push(c->pages.data() + p0, p1 - p0);
+      cs::Meta m;
+      if ((st = place_meta(p, b, &m)) != CS_OK) break;
+      st = timed_launch(p, CS_PROF_UNPACK, "unpack launch", [&] {
+        if (p->fp4)
+          return cs::launch_unpack_fp4(p->geom(), src, m, cs::ConvTable::slot_of(h), n_tokens, static_cast<int>(p0),
+                                       static_cast<int>(p1 - p0), p->stream);
+        return cs::launch_unpack(p->geom(), src, m, cs::ConvTable::slot_of(h),
+                                 n_tokens, static_cast<int>(p0), static_cast<int>(p1 - p0), p->stream);
+      });
+    }
+  } catch (...) {
+    st = out_of_memory();
   }
+  if (st != CS_OK) {   // (launches already issued write pages that are free again, before whoever takes them next)
+    p->pages.unalloc(c->pages);
+    c->pages.clear();
+    p->convs.destroy(h, p->pages);
+    return st;
+  }
+  *out_conv = h;
   return CS_OK;
 } CS_NO_THROW
 
