@@ -170,8 +170,9 @@ cs_status cs_kv_append_batch(cs_pool* pool, int32_t n_convs, const cs_conv* conv
  * conversation's first token), pair i = 0 .. rotary_dim/2 - 1 by p inv_freq[i] radians:
  *   (a, b) -> amplitude (a cos - b sin, a sin + b cos)
  * where a pair is dims (i, i + rotary_dim/2), or (2 i, 2 i + 1) with interleaved; the other dims stay.
- * The angle is exact to 2^-34 turns at any position; the rotated value is computed in fp32 and rounded
- * once, to bf16 or to the pool's 4 bits.
+ * The angle, kept as a 64-bit fraction of a turn and rounded to fp32, is within 2^-25 turns of the exact
+ * one at any position. The rotated value is computed in fp32, within 2^-21 amplitude (|a| + |b|), and
+ * rounded once, to bf16 or to the pool's 4 bits.
  */
 typedef struct {
   int32_t rotary_dim;   /* 16, 32, .., head_dim */

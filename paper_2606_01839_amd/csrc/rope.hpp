@@ -1,9 +1,11 @@
 // Rotary positions on the device: angles, and the rotation of rows of heads.
 //
 // Pair i of a row at position p turns by p f_i radians. f_i / 2 pi is kept as a 64-bit fraction of a turn,
-// so p times it, modulo 2^64, is the angle's fraction of a turn exactly (p < 2^31: to 2^-34 turns; in fp32
-// the angle of position 10^5 would be off by 4e-3 radians). Its upper 32 bits, signed, are within half a turn of zero,
-// where v_sin_f32 and v_cos_f32, which take turns, are within 1.9e-7 (measured over 4 million angles).
+// so p times it, modulo 2^64, is the angle's fraction of a turn to 2^-34 at any p < 2^31 (in fp32
+// the angle of position 10^5 would be off by 4e-3 radians). Its upper 32 bits, signed, are within half a turn of zero;
+// rounded to fp32 they are off by up to 2^-26 turns (9.4e-8 radians) and 2^-32, and v_sin_f32 and v_cos_f32, which
+// take turns, by 1.9e-7 (measured over 4 million angles). With the fp32 arithmetic a rotated value is within
+// 2^-21 = 4.8e-7 of |a| + |b| before it is rounded (measured where the terms cancel: 2.0e-7).
 #pragma once
 
 #include "device_common.hpp"
