@@ -109,7 +109,9 @@ cs_status cs_pool_create(const cs_pool_desc* desc, void* kv_base, size_t kv_byte
  *   e2m1 value times it (ties to the even code) and at most to 6 times it. K and V must be finite: a group
  *   with an infinity or NaN is held, read back and attended as NaN. Attention is that of the held values:
  *   every call below does on such a pool what it does on a bf16 one, with the same arguments, asynchrony and
- *   errors.
+ *   errors. Scores take a query as three 3-bit parts for every 32 dims (head_dim 64, decode: 16 dims): exactly
+ *   where its magnitude is at least 2^-8 of the largest of them, else to within 2^-16 of that largest, so a
+ *   query with outliers far over the dims that matter loses bits that a bf16 pool keeps.
  *   Block (layer, page, kv head), two codes a byte, the first in the low bits: K[d/32 groups][16 tokens][32
  *   dims], V[4][16][d/16][4]: part i, row c, tile t hold dim 16 t + c of tokens 4 i .. 4 i + 3; then bytes e
  *   (the power 2^(e - 127); 255: NaN, V's codes then zeros): K[16 tokens][d/32 groups], V[16 tokens], zeros
