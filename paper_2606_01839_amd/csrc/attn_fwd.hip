@@ -32,8 +32,9 @@
 // 128 of which 0.5 is the plan, 1.5 pages, queries and first copies, 1.0 their arrival, 2.5 the first
 // tile (mask, weights taken twice) and 2.0-3.7 were 8-byte output stores into 32 rows at a time.
 // Over 4-bit pages (fp4.hpp) a launch is bound by the same, with 3/4 of the score product's matrix time and the conversion
-// of V beside it: eight conversations' 128-2048 tokens on 8k-40k 1451-1525 us (1.20-1.26 PFLOP/s; bf16 pages 1598), 301
-// tokens on 41k 175-182 (217); at head dim 64 the softmax leaves no difference (111 us against 109).
+// of V beside it: eight conversations' 128-2048 tokens on 8k-40k 1451-1550 us (1.18-1.26 PFLOP/s; in turn with bf16 pages
+// 1472 against 1626), 301 tokens on 41k 175-182 (178 against 189). At head dim 64 the softmax leaves little difference (109
+// us against 111): vector units busy 63% of the time, matrix cores 31%, hardly at a time.
 // Head dim 64 against a kernel that staged tiles through registers, one wave per SIMD: six prompts of
 // 300-9000 tokens 361 -> 229 us.
 #include <cfloat>
@@ -437,7 +438,9 @@ __device__ __forceinline__ void attn_fwd_block(const ExtendArgs& a, const int bl
 #pragma unroll
         for (int kt2 = 0; kt2 < 2; ++kt2) s[kt2] = mx_score<2, 2>(kmx[1][kt2], kmx_s[kt2], query[1], s[kt2]);
       }
-      // the conversion of tile j+2 goes between the score products, which leave the vector units free
+      // The conversion of tile j+2 goes between the score products, which leave the vector units free, where the
+      // operands were read ahead. Without PRE the registers hold K of one key half at a time: the compiler has its three
+      // products, the read of the other half's and their products, then the conversion.
       feed(buf);
 #pragma unroll
       for (int i = 0; i < 6 * KM; ++i) {

@@ -322,7 +322,8 @@ __device__ __forceinline__ void split_body(const DecodeArgs& a, const int work, 
   // l_run holds this lane's keys only; sum over the four k-blocks of the column.
   l_run += xor_shfl(l_run, 16);
   l_run += xor_shfl(l_run, 32);
-  // A wave past the conversation's end has m = -inf, l = 0, o = 0 and adds nothing below.
+  // A wave past the conversation's end has l = 0 and o = 0 and adds nothing below, whatever its weight: its m, -inf (4-bit
+  // pages: -FLT_MAX), is no more than M, so the weight is finite.
   if (wave > 0 && c < a.group) {
     float* x = xch + ((wave - 1) * 8 + c) * (D + 2);
 #pragma unroll

@@ -123,11 +123,16 @@ DecodePlan plan_decode_filling(const std::vector<int32_t>& slots, const std::vec
                                int32_t n_kv_heads, int64_t target_items, int32_t n_cus);
 
 // The same for 4-bit pages, where an item reads 3.8 times fewer bytes and its start-up weighs as much more:
-// items of more than one round of the CUs are made longer, in steps of a page pair, until they fit one (splits
-// up to 512 keys) or else two, which the CUs hold at a time (up to 384). 32 query and 8 kv heads of 128: one
-// conversation of 60k tokens 23.2 -> 18.3 us, 100k 35.7 -> 24.0, eight of 1k-9k 19.0 -> 17.0, sixteen 30.3 -> 25.6, 64 of
-// 300-2000 27.0 -> 20.6 (every one a single item); beyond those limits the time of an item is longer than what is
-// saved (sixteen of 8k-32k: 66.2 us with 512-key splits, 74.1 with 1024).
+// items of more than one round of the CUs are made longer, in steps of a page pair and by one at least, until they fit
+// one (splits up to 512 keys) or else two, which the CUs hold at a time in the decode's own launch (up to 384). 32 query
+// and 8 kv heads of 128: one conversation of 60k tokens 23.2 -> 18.3 us, 100k 35.7 -> 24.0, eight of 1k-9k 19.0 -> 17.0,
+// sixteen 30.3 -> 25.6, 64 of 300-2000 27.0 -> 20.6 (every one a single item); beyond those limits the time of an item is
+// longer than what is saved (sixteen of 8k-32k: 66.2 us with 512-key splits, 74.1 with 1024). Items that fit two rounds as
+// they are get the one step too, which saves no round: 1% faster to 4% slower (one conversation of 20k beside 32 of 900
+// 20.4 -> 20.7 us, 40k beside 24 of 1000 22.3 -> 22.1, one of 3000 beside 55 of 300-900 19.0 -> 19.7).
+// A layer-ordered mixed step takes the same plan, though its launch holds one workgroup a CU: with the second search left
+// out 16 conversations of 1k-9k beside a 513-token chunk take 119 us a layer instead of 131, 64 beside two chunks 308
+// instead of 280.
 DecodePlan plan_decode_rounds(const std::vector<int32_t>& slots, const std::vector<int64_t>& lens,
                               int32_t n_kv_heads, int64_t target_items, int32_t n_cus);
 
