@@ -842,7 +842,9 @@ hipError_t launch_extend(const PoolGeom& g, int layer, int n_layers, const Exten
   const ExtendArgs a = make_extend_args(g, layer, e, q, out, parts);
   LaunchMeta m;
   fill_meta(e.meta, &m);
-  const dim3 grid(e.n_tiles * g.n_kv_heads, n_layers);
+  const int64_t blocks = static_cast<int64_t>(e.n_tiles) * g.n_kv_heads;
+  if (!grid_holds(blocks, 512)) return hipErrorInvalidConfiguration;
+  const dim3 grid(static_cast<unsigned>(blocks), n_layers);
   // At head_dim 64 a launch of more than 2.5 workgroups per CU runs two at a time on each: one prompt of
   // 9000 tokens (1128 workgroups) 352 -> 339 us, 6000 (752) 168 -> 163; below, one at a time that reads
   // its operands ahead is the faster form: 4500 (568) 98 against 106 us, 2500 (320) 41 against 45. A
@@ -899,7 +901,9 @@ hipError_t launch_mixed_layer(const PoolGeom& g, int layer, const ExtendLaunch& 
   // end later. 64 conversations of 1k-9k beside chunks of 700 on 8k and 64 on 3k, 32 layers: 10.3 -> 5.9 ms, seven other
   // steps 1-9% faster or the same within 2%.)
   const int n_mix = e.n_tiles + (e.n_merges > 0 && !g.fp4 ? w.n_items * 6 / 10 : 0);
-  const int blocks = (e.n_tiles + w.n_items) * g.n_kv_heads;
+  const int64_t n_blocks = (static_cast<int64_t>(e.n_tiles) + w.n_items) * g.n_kv_heads;
+  if (!grid_holds(n_blocks, 512)) return hipErrorInvalidConfiguration;
+  const int blocks = static_cast<int>(n_blocks);
   return by_shape(g, [&](auto d, auto grp) {
     if (g.fp4 && e.chained) mixed_fp4_kernel<d(), grp(), true><<<blocks, 512, 0, stream>>>(ea, e.n_tiles, n_mix, da);
     else if (g.fp4) mixed_fp4_kernel<d(), grp(), false><<<blocks, 512, 0, stream>>>(ea, e.n_tiles, n_mix, da);
@@ -913,8 +917,10 @@ hipError_t launch_mixed_merge(const PoolGeom& g, const ExtendLaunch& e, void* ou
                               const DecodeLaunch& w, const float* partials, void* out_dec, hipStream_t stream) {
   // out_dec == nullptr: the split wrote the decode outputs
   const int n_ext = e.n_merges * g.n_kv_heads * 8;
-  const int blocks = n_ext + (out_dec != nullptr ? w.n_convs * g.n_q_heads : 0);
-  if (blocks == 0) return hipSuccess;
+  const int64_t n_blocks = n_ext + (out_dec != nullptr ? static_cast<int64_t>(w.n_convs) * g.n_q_heads : 0);
+  if (n_blocks == 0) return hipSuccess;
+  if (!grid_holds(n_blocks, 256)) return hipErrorInvalidConfiguration;
+  const int blocks = static_cast<int>(n_blocks);
   if (e.meta.dev == nullptr || w.meta.dev == nullptr || (n_ext > 0 && parts == nullptr)) return hipErrorInvalidValue;
   const ExtendArgs ea = make_extend_args(g, 0, e, nullptr, out_ext, parts);
   const DecodeArgs da = make_decode_args(g, 0, w, nullptr, out_dec, partials);

@@ -87,9 +87,11 @@ hipError_t launch_decode_split(const PoolGeom& g, int layer, int n_layers, const
   DecodeArgs a = make_decode_args(g, layer, w, q, direct_out, partials);
   a.direct = direct_out != nullptr && w.n_items == w.n_convs;
   if (direct_out != nullptr && !a.direct) return hipErrorInvalidValue;
+  const int64_t blocks = static_cast<int64_t>(w.n_items) * g.n_kv_heads;
+  if (!grid_holds(blocks, kDecodeItemThreads)) return hipErrorInvalidConfiguration;
   LaunchMeta m;
   fill_meta(w.meta, &m);
-  const dim3 grid(w.n_items * g.n_kv_heads, n_layers);
+  const dim3 grid(static_cast<unsigned>(blocks), n_layers);
   if (g.head_dim == 128 && g.fp4) decode_split_fp4_kernel<128><<<grid, kDecodeItemThreads, 0, stream>>>(m, a);
   else if (g.head_dim == 64 && g.fp4) decode_split_fp4_kernel<64><<<grid, kDecodeItemThreads, 0, stream>>>(m, a);
   else if (g.head_dim == 128) decode_split_kernel<128><<<grid, kDecodeItemThreads, 0, stream>>>(m, a);
@@ -102,10 +104,12 @@ hipError_t launch_decode_merge(const PoolGeom& g, int n_layers, const DecodeLaun
                                void* out, hipStream_t stream) {
   if (w.n_convs == 0 || n_layers == 0) return hipSuccess;
   if (!w.meta.ok()) return hipErrorInvalidValue;
+  const int64_t blocks = static_cast<int64_t>(w.n_convs) * g.n_q_heads;
+  if (!grid_holds(blocks, 256)) return hipErrorInvalidConfiguration;
   const DecodeArgs a = make_decode_args(g, 0, w, nullptr, out, partials);
   LaunchMeta m;
   fill_meta(w.meta, &m);
-  const dim3 grid(w.n_convs * g.n_q_heads, n_layers);
+  const dim3 grid(static_cast<unsigned>(blocks), n_layers);
   if (g.head_dim == 128) decode_merge_kernel<128><<<grid, 256, 0, stream>>>(m, a);
   else if (g.head_dim == 64) decode_merge_kernel<64><<<grid, 256, 0, stream>>>(m, a);
   else return hipErrorInvalidValue;

@@ -21,6 +21,10 @@ struct PoolGeom {
   bool fp4;             // blocks of 4-bit codes and scales (fp4.hpp) instead of bf16
 };
 
+// Whether a grid holds that many workgroups in x: fewer than 2^32 threads (a launch of more runs some of them and reports
+// no error). Launches whose count grows with a batch return hipErrorInvalidConfiguration where it does not.
+inline bool grid_holds(int64_t workgroups, int threads) { return workgroups * threads < (int64_t(1) << 32); }
+
 // Metadata of one launch (descriptors, work lists, page ids): `bytes` bytes laid out on the host at
 // `host`, or already on the device at `dev` (a stream-ordered upload; `host` is then unused). A plan
 // of at most kMetaBytes travels in the launch's own kernel arguments (dev = nullptr): an upload is a
@@ -92,8 +96,7 @@ int rope_q_layers(const PoolGeom& g);
 hipError_t launch_read(const PoolGeom& g, const Meta& meta, int n_chunks, void* k, void* v, int64_t dst_rows, hipStream_t stream);
 
 // Pack of logical pages [lp0, lp0 + n_lp) of a conversation (of a pool of either kind) into the wire of a 4-bit
-// pool, and that pool's unpack. A launch takes at most kMaxPackPages (256 threads a page, and a grid has fewer
-// than 2^32).
+// pool, and that pool's unpack. A launch takes at most kMaxPackPages (256 threads a page).
 constexpr int kMaxPackPages = (1 << 24) - 1;
 hipError_t launch_pack_fp4(const PoolGeom& g, int slot, int64_t len, int lp0, int n_lp, void* wire, hipStream_t stream);
 hipError_t launch_unpack_fp4(const PoolGeom& g, const void* wire, const Meta& meta, int slot, int64_t len, int lp0, int n_lp,
