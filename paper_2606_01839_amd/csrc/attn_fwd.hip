@@ -505,7 +505,7 @@ __device__ __forceinline__ void attn_fwd_block(const ExtendArgs& a, const int bl
       return ps0 + ps1;
     };
     float ps = weights(c, -m_s);
-    if (far || __builtin_amdgcn_ballot_w64(!(ps <= kSumLimit)) != 0) {
+    if (__builtin_expect(far, false) || __builtin_amdgcn_ballot_w64(!(ps <= kSumLimit)) != 0) {
       float mx = -INFINITY;
 #pragma unroll
       for (int kt2 = 0; kt2 < 2; ++kt2)
@@ -520,7 +520,7 @@ __device__ __forceinline__ void attn_fwd_block(const ExtendArgs& a, const int bl
       float w_scale = c, w_off = -m_new;
       // (-FLT_MAX: a row that has seen no key)
       far = __builtin_amdgcn_ballot_w64(m_new > -FLT_MAX && __builtin_fabsf(m_new) >= kFarScore) != 0;
-      if (far) {
+      if (__builtin_expect(far, false)) {
 #pragma clang fp contract(off)
 #pragma unroll
         for (int kt2 = 0; kt2 < 2; ++kt2)
