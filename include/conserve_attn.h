@@ -18,8 +18,8 @@
  *    stream reaches the call. Host pointers: cs_conv arrays, q_lens, and the out-parameters.
  *  - Element type: bf16 (IEEE binary32 with the low 16 bits dropped) everywhere; accumulation fp32.
  *    A pool may hold K and V in 4 bits instead (cs_pool_create_as); what goes in and out stays bf16.
- *  - Append-then-attend: cs_kv_append is the only writer of a conversation's K/V. Attention calls
- *    take queries for the LAST q_len positions of each conversation; query i of a conversation of
+ *  - Append-then-attend: cs_kv_append is the only writer of a conversation's K/V. Attention calls (but for cs_attn_tree
+ *    and cs_attn_cross) take queries for the LAST q_len positions of each conversation; query i of a conversation of
  *    length L sits at position p = L - q_len + i and sees keys 0..p (itself included). Softmax
  *    scale is exactly 1/sqrt(head_dim). Query head h reads KV head h / (n_q_heads / n_kv_heads).
  *  - Errors: every call validates all arguments before changing any state; on error it returns a
@@ -261,6 +261,55 @@ cs_status cs_attn_extend(cs_pool* pool, int32_t n_convs, const cs_conv* convs,
                          cs_stream stream);
 
 /*
+ * Attention of drafted tokens over the cache that holds them, to verify them in one call (a step of several guesses in
+ * place of one token). The last q_lens[i] tokens of conversation i are a tree: parents[..], one for each query row in batch
+ * order, is -1 (the token follows the last cached one) or the index of an earlier token of the same tree, counted from
+ * its first. Row j sees the length - q_lens[i] cached tokens, its ancestors and itself, and no other branch: a NaN or infinity in
+ * a branch it does not see (keys or values) does not reach it. A tree that is a chain (parents -1, 0, 1, ..) is cs_attn_extend.
+ * At most CS_MAX_DRAFT tokens a tree. Pages of either format. Several lengths, and none, in one batch are fine.
+ * q, out: device [sum(q_lens)][n_q_heads][head_dim] bf16. Deterministic and independent of page placement; a row's last bits
+ * depend on the batch, as with cs_attn_extend. May be captured into a graph, as cs_attn_decode_batch_noalloc.
+ * Errors: as cs_attn_extend; CS_ERANGE (a tree too large), CS_EINVAL (null parents, a parent that is no earlier token).
+ */
+#define CS_MAX_DRAFT 1024
+cs_status cs_attn_tree(cs_pool* pool, int32_t n_convs, const cs_conv* convs, const int32_t* q_lens, const int32_t* parents,
+                       int32_t layer, const void* q, void* out, cs_stream stream);
+
+/*
+ * cs_kv_append_rope for the drafted tokens of such trees: token j of conversation i takes the next slot, as with any
+ * append, but turns by its position in the tree, length + depth (depth 0 for a parent of -1), and so does its query. `parents`
+ * as in cs_attn_tree, one for each new token. (Without rotary positions cs_kv_append_batch appends a draft.)
+ * Errors: as cs_kv_append_rope; CS_ERANGE and CS_EINVAL for the trees, as cs_attn_tree.
+ */
+cs_status cs_kv_append_tree(cs_pool* pool, const cs_rope* rope, int32_t n_convs, const cs_conv* convs, const int32_t* n_new,
+                            const int32_t* parents, const void* k, const void* v, const void* q, void* q_out, cs_stream stream);
+
+/*
+ * Keep the accepted tokens of a draft: of the last n_last[i] tokens of conversation i those stay whose indexes (0 for
+ * the first of them) the next n_keep[i] entries of `keep` give, increasing, and follow the tokens before them in that order; the
+ * others are dropped, and pages that end up empty return to the pool. Of a tree the indexes are those of an accepted path:
+ * its tokens were turned by their depth, which is now their slot. n_keep = 0 takes the conversation back to what it was before
+ * its last n_last tokens, whatever they were; n_keep == n_last changes nothing. All layers; pages of either format, whose
+ * bytes move as they are. Where the kept tokens are the first ones nothing moves.
+ * After CS_EHIP the last n_last tokens are undefined, the lengths unchanged. Not under stream capture (CS_ESTATE).
+ * Errors: CS_EINVAL (null, duplicate conversation, n_keep not in 0 .. n_last, keep not increasing in 0 .. n_last - 1),
+ * CS_ENOENT, CS_ESTATE (n_last > length), CS_ENOMEM (more moved tokens than a metadata upload holds, some 500,000), CS_EHIP.
+ */
+cs_status cs_kv_keep(cs_pool* pool, int32_t n_convs, const cs_conv* convs, const int32_t* n_last, const int32_t* n_keep,
+                     const int32_t* keep, cs_stream stream);
+
+/*
+ * Cross attention: q_lens[i] rows see ALL tokens of conversation i, which holds the K and V of an encoder's states (or any other
+ * context), appended like any tokens. No mask, no relation between a row and a position: any number of rows, more
+ * than the conversation has tokens too, one for each of several hypotheses or a whole text. A conversation may appear several
+ * times in a batch (rows of its entries are computed one by one; as one entry they share the reading). Rows of a conversation
+ * without tokens are zeros. q, out, the result's bits, and capture: as cs_attn_tree.
+ * Errors: CS_EINVAL (null, q_len < 0, too many rows), CS_ENOENT, CS_ERANGE (layer), CS_ENOMEM, CS_EHIP.
+ */
+cs_status cs_attn_cross(cs_pool* pool, int32_t n_convs, const cs_conv* convs, const int32_t* q_lens, int32_t layer, const void* q,
+                        void* out, cs_stream stream);
+
+/*
  * Batched single-token decode (Section 2.1 / 3.2: each step reads the whole cache of every
  * conversation in the batch; memory-bound). The query of convs[i] is its last position.
  * q, out: device [n_convs][n_q_heads][head_dim] bf16. Conversations distinct, length >= 1.
@@ -401,7 +450,8 @@ enum {
   CS_PROF_ATTN_FWD = 5,      /* prefill / extend attention kernel and the merge of cut tiles */
   CS_PROF_MIXED_LAYER = 6,   /* one layer's extend tiles + decode split in one launch */
   CS_PROF_KINDS = 7
-  /* queries rotated by cs_rope_q count as CS_PROF_APPEND, cs_kv_read as CS_PROF_UNPACK */
+  /* queries rotated by cs_rope_q and cs_kv_keep count as CS_PROF_APPEND, cs_kv_read as CS_PROF_UNPACK, cs_attn_tree
+   * and cs_attn_cross as CS_PROF_ATTN_FWD */
 };
 cs_status cs_profile_start(cs_pool* pool);
 cs_status cs_profile_stop(cs_pool* pool, double* ms, int64_t* launches);

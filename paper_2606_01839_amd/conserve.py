@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import array
 import ctypes
+import itertools
 import os
 
 import numpy as np
@@ -26,6 +27,7 @@ CS_KV_BF16, CS_KV_FP4 = 0, 1  # cs_pool_create_as
 KV_FORMATS = {"bf16": CS_KV_BF16, "fp4": CS_KV_FP4}
 ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "parts": 3}   # CS_ROPE_*
 WIRE_FP4_VERSION = 1          # CS_WIRE_FP4_VERSION: the frozen layout of kv_pack_fp4
+MAX_DRAFT = 1024              # CS_MAX_DRAFT: tokens a tree of drafts may have
 WIRE_FORMAT_VERSION = 1       # CS_WIRE_FORMAT_VERSION: the frozen layout of kv_pack / kv_unpack
 
 EXPORTS = [
@@ -34,7 +36,7 @@ EXPORTS = [
     "cs_kv_append", "cs_kv_append_batch", "cs_attn_prefill_turn1", "cs_attn_extend",
     "cs_attn_decode_batch", "cs_attn_decode_batch_noalloc", "cs_mixed_step", "cs_kv_pack_size", "cs_kv_pack", "cs_kv_unpack",
     "cs_pool_kv_bytes_as", "cs_pool_create_as", "cs_rope_init", "cs_kv_append_rope", "cs_rope_q", "cs_kv_read", "cs_mixed_step_rope",
-    "cs_kv_pack_fp4_size", "cs_kv_pack_fp4",
+    "cs_kv_pack_fp4_size", "cs_kv_pack_fp4", "cs_attn_tree", "cs_kv_append_tree", "cs_kv_keep", "cs_attn_cross",
     "cs_profile_start",
     "cs_profile_stop", "cs_device_info", "cs_probe_stream_read", "cs_debug_fail_launches",
     "cs_last_error",
@@ -103,6 +105,10 @@ def load_library(path: str = _LIB_PATH) -> ctypes.CDLL:
         "cs_rope_q": (I32, [P, ctypes.POINTER(RopeDesc), I32, VP, VP, I32, VP, VP, VP]),
         "cs_mixed_step_rope": (I32, [P, ctypes.POINTER(RopeDesc), I32, VP, VP, I32, VP, VP, VP, VP, VP, VP, VP,
                                      ctypes.c_uint32, VP]),
+        "cs_attn_tree": (I32, [P, I32, VP, VP, VP, I32, VP, VP, VP]),
+        "cs_kv_append_tree": (I32, [P, ctypes.POINTER(RopeDesc), I32, VP, VP, VP, VP, VP, VP, VP, VP]),
+        "cs_kv_keep": (I32, [P, I32, VP, VP, VP, VP, VP]),
+        "cs_attn_cross": (I32, [P, I32, VP, VP, I32, VP, VP, VP]),
         "cs_kv_read": (I32, [P, I32, VP, VP, VP, VP, VP, VP]),
         "cs_kv_pack_fp4_size": (I32, [P, I32, ctypes.POINTER(SZ)]),
         "cs_kv_pack_fp4": (I32, [P, I32, VP, SZ, VP]),
@@ -160,6 +166,13 @@ def _i32_array(xs):
     except TypeError:           # not all integers: numpy's conversion
         a = array.array("i", np.asarray(xs, dtype=np.int32).reshape(-1).tolist())
     return a, a.buffer_info()[0]
+
+
+def _lists_array(lists, lens, name):
+    """(int32 array, address) of one list for each conversation, of the given lengths, end to end."""
+    if [len(x) for x in lists] != list(lens):
+        raise ValueError(f"{name} must have one list for each conversation, of lengths {list(lens)}")
+    return _i32_array(list(itertools.chain.from_iterable(lists)))
 
 
 def _stream_handle(device: torch.device):
@@ -376,6 +389,42 @@ class KVPool:
                                           _stream_handle(self.device)))
         return q_out
 
+    def kv_append_tree(self, convs, n_new, parents, k: torch.Tensor, v: torch.Tensor, rope: Rope, q: torch.Tensor | None = None,
+                       q_out: torch.Tensor | None = None):
+        """kv_append_rope of drafted tokens: token j of a conversation turns by its position in the tree, length + depth.
+        ``parents``: one list for each conversation, parents[i][j] = -1 (after the last cached token) or an earlier
+        token of the tree. Returns q_out."""
+        ca, cp = _i32_array(convs)
+        na, npp = _i32_array(n_new)
+        if len(ca) != len(na):
+            raise ValueError("convs and n_new differ in length")
+        pa, pp = _lists_array(parents, na, "parents")
+        shp = (self.n_layers, sum(na), self.n_kv_heads, self.head_dim)
+        kp, vp = self._dev(k, "k", shp), self._dev(v, "v", shp)
+        qp = op = None
+        if q is not None:
+            qshp = (self.n_layers, sum(na), self.n_q_heads, self.head_dim)
+            qp = self._dev(q, "q", qshp)
+            if q_out is None:
+                q_out = torch.empty_like(q)
+            op = self._rotated(q, q_out, "q_out", qshp)
+        elif q_out is not None:
+            raise ValueError("q_out without q")
+        _check(self.lib.cs_kv_append_tree(self._handle, ctypes.byref(rope.desc), len(ca), cp, npp, pp, kp, vp, qp, op,
+                                          _stream_handle(self.device)))
+        return q_out
+
+    def kv_keep(self, convs, n_last, keep) -> None:
+        """Of the last n_last[i] tokens of each conversation keep those with the increasing indexes keep[i] (of an accepted
+        path of a tree), in that order, and drop the others; keep[i] = [] drops them all."""
+        ca, cp = _i32_array(convs)
+        la, lp = _i32_array(n_last)
+        if not len(ca) == len(la) == len(keep):
+            raise ValueError("convs, n_last and keep differ in length")
+        na, npp = _i32_array([len(x) for x in keep])
+        ka, kp = _lists_array(keep, na, "keep")
+        _check(self.lib.cs_kv_keep(self._handle, len(ca), cp, lp, npp, kp, _stream_handle(self.device)))
+
     def rope_q(self, convs, q_lens, q: torch.Tensor, rope: Rope, out: torch.Tensor | None = None) -> torch.Tensor:
         """Queries of the last q_lens[i] positions of each conversation, rotated: q [rows][n_q_heads][head_dim]
         or [any layers][rows][n_q_heads][head_dim]; out may be q itself."""
@@ -423,11 +472,15 @@ class KVPool:
         return k, v
 
     # -- attention -----------------------------------------------------------------------------
-    def _attend(self, fn, convs, q_lens, layer, q, out):
+    def _attend(self, fn, convs, q_lens, layer, q, out, parents=None):
         ca, cp = _i32_array(convs)
         qa, qp = _i32_array(q_lens)
         if len(ca) != len(qa):
             raise ValueError("convs and q_lens differ in length")
+        trees = ()
+        if parents is not None:
+            pa, pp = _lists_array(parents, qa, "parents")
+            trees = (pp,)
         shp = (sum(qa), self.n_q_heads, self.head_dim)
         qptr = self._dev(q, "q", shp)
         if out is None:
@@ -435,7 +488,7 @@ class KVPool:
             optr = out.data_ptr()
         else:
             optr = self._dev(out, "out", shp)
-        _check(fn(self._handle, len(ca), cp, qp, layer, qptr, optr, _stream_handle(self.device)))
+        _check(fn(self._handle, len(ca), cp, qp, *trees, layer, qptr, optr, _stream_handle(self.device)))
         return out
 
     def attn_prefill_turn1(self, convs, q_lens, layer, q, out=None) -> torch.Tensor:
@@ -443,6 +496,17 @@ class KVPool:
 
     def attn_extend(self, convs, q_lens, layer, q, out=None) -> torch.Tensor:
         return self._attend(self.lib.cs_attn_extend, convs, q_lens, layer, q, out)
+
+    def attn_tree(self, convs, q_lens, parents, layer, q, out=None) -> torch.Tensor:
+        """Attention of drafted tokens, the last q_lens[i] of each conversation: row j sees the tokens before them, its
+        ancestors and itself. ``parents``: one list for each conversation, -1 (after the last cached token) or an
+        earlier token of the tree."""
+        return self._attend(self.lib.cs_attn_tree, convs, q_lens, layer, q, out, parents)
+
+    def attn_cross(self, convs, q_lens, layer, q, out=None) -> torch.Tensor:
+        """Cross attention: q_lens[i] rows see every token of convs[i] (an encoder's states). A conversation may appear
+        several times, have fewer tokens than rows, or none (zeros)."""
+        return self._attend(self.lib.cs_attn_cross, convs, q_lens, layer, q, out)
 
     def attn_decode_batch(self, convs, layer, q, out=None) -> torch.Tensor:
         return self._decode(self.lib.cs_attn_decode_batch, convs, layer, q, out)

@@ -394,7 +394,7 @@ cs::Meta meta_part(const void* dev, size_t off, size_t bytes) {
   return m;
 }
 
-cs_status check_convs(cs_pool* p, int32_t n, const cs_conv* convs, std::vector<const cs::Conv*>& out) {
+cs_status check_convs(cs_pool* p, int32_t n, const cs_conv* convs, std::vector<const cs::Conv*>& out, bool distinct = true) {
   if (n < 0) return fail(CS_EINVAL, "negative batch size");
   if (n > 0 && !convs) return fail(CS_EINVAL, "null conversation array");
   out.clear();
@@ -410,7 +410,7 @@ cs_status check_convs(cs_pool* p, int32_t n, const cs_conv* convs, std::vector<c
     const cs::Conv* c = p->convs.find(convs[i]);
     if (!c) return fail(CS_ENOENT, "unknown conversation handle " + std::to_string(convs[i]));
     uint32_t& mark = p->seen[static_cast<size_t>(cs::ConvTable::slot_of(convs[i]))];
-    if (mark == p->batch)
+    if (distinct && mark == p->batch)
       return fail(CS_EINVAL, "conversation " + std::to_string(convs[i]) + " appears twice in a batch");
     mark = p->batch;
     out.push_back(c);
@@ -673,6 +673,7 @@ struct RotatedAppend {
   cs::RopeArgs rope;
   const void* q = nullptr;   // may be null
   void* q_out = nullptr;
+  const int32_t* depths = nullptr;   // of the new tokens in their trees: token i turns by (length before) + depths[i]
 };
 
 // Rows a query rotation takes at most: 16 a workgroup of 256, and a grid has fewer than 2^32 threads.
@@ -685,13 +686,15 @@ cs_status check_rope_q(int64_t rows, size_t n_convs) {
   return CS_OK;
 }
 
-// Queries [n_layers][rows][n_q_heads][head_dim] rotated in launches of their own.
+// Queries [n_layers][rows][n_q_heads][head_dim] rotated in launches of their own. `pos` (may be null): every row's
+// position, in place of `convs`.
 cs_status run_rope_q(cs_pool* p, const std::vector<cs::RopeConv>& convs, int64_t rows, int32_t n_layers, const cs::RopeArgs& rope,
-                     const void* q, void* out) {
+                     const void* q, void* out, const std::vector<int32_t>* pos = nullptr) {
   cs_status st = check_rope_q(rows, convs.size());
   if (st != CS_OK) return st;
   Blob b;
-  b.push(convs.data(), convs.size());
+  if (pos) b.push(pos->data(), pos->size());
+  else b.push(convs.data(), convs.size());
   cs::Meta m;
   st = place_meta(p, b, &m);
   const cs::PoolGeom g = p->geom();
@@ -763,17 +766,37 @@ cs_status append_impl(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t
     const std::vector<cs::PageChunk> chunks = cs::plan_append(slots, old_lens, nn, lists);
     const cs::PoolGeom g = p->geom();
     const size_t carry_bytes = carry ? carry->bytes.size() : 0;
-    const bool q_apart = rotated && rotated->q && cs::append_rope_groups(g, chunks.size()) > kRopeApartGroups;
-    auto launch = [&](const cs::Meta& m, int n_chunks, const cs::AppendCarry& c) {
+    const int32_t* depths = rotated ? rotated->depths : nullptr;
+    const size_t chunk_bytes = sizeof(cs::PageChunk) + (depths ? cs::kPage * sizeof(int32_t) : 0);
+    // (a tree's queries in a launch of their own: their rows' positions are one upload)
+    const bool q_apart = rotated && rotated->q && cs::append_rope_groups(g, chunks.size()) > kRopeApartGroups &&
+                         (!depths || total * sizeof(int32_t) <= kQuarter);
+    auto launch = [&](const cs::Meta& m, int n_chunks, const cs::AppendCarry& c, size_t pos_off = 0) {
       return timed_launch(p, CS_PROF_APPEND, "append launch", [&] {
         if (rotated)
           return cs::launch_append_as(g, m, n_chunks, c, &rotated->rope, k, v, q_apart ? nullptr : rotated->q, rotated->q_out, total,
-                                      p->stream);
-        if (p->fp4) return cs::launch_append_as(g, m, n_chunks, c, nullptr, k, v, nullptr, nullptr, total, p->stream);
+                                      pos_off, p->stream);
+        if (p->fp4) return cs::launch_append_as(g, m, n_chunks, c, nullptr, k, v, nullptr, nullptr, total, 0, p->stream);
         return cs::launch_append(g, m, n_chunks, c, k, v, total, p->stream);
       });
     };
-    if (chunks.size() * sizeof(cs::PageChunk) + carry_bytes <= cs::kMetaBytes) {
+    if (depths) {
+      // Chunks in parts of one upload (or launch argument) each, the positions of a chunk's 16 slots behind them.
+      const size_t per = kQuarter / chunk_bytes - 1;
+      for (size_t c0 = 0; c0 < chunks.size() && st == CS_OK; c0 += per) {
+        const size_t c1 = std::min(chunks.size(), c0 + per);
+        std::vector<int32_t> at((c1 - c0) * cs::kPage);
+        for (size_t c = c0; c < c1; ++c)
+          for (int32_t t = chunks[c].t0; t < chunks[c].t1; ++t)
+            at[(c - c0) * cs::kPage + t] =
+                static_cast<int32_t>(old_lens[static_cast<size_t>(chunks[c].conv)]) + depths[chunks[c].src_row + t - chunks[c].t0];
+        Blob b;
+        b.push(chunks.data() + c0, c1 - c0);
+        const size_t pos_off = b.push(at.data(), at.size());
+        cs::Meta m;
+        if ((st = place_meta(p, b, &m)) == CS_OK) st = launch(m, static_cast<int>(c1 - c0), {}, pos_off);
+      }
+    } else if (chunks.size() * sizeof(cs::PageChunk) + carry_bytes <= cs::kMetaBytes) {
       // small: the chunks travel in the launch's arguments, and so does the metadata of the launches
       // that follow, which the append kernel stores to the ring's device half.
       Blob b;
@@ -807,12 +830,16 @@ cs_status append_impl(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t
     }
     if (q_apart && st == CS_OK) {
       std::vector<cs::RopeConv> rc;
+      std::vector<int32_t> pos;
       int32_t row = 0;
       for (int32_t i = 0; i < n; ++i) {
-        if (nn[i] > 0) rc.push_back({row, static_cast<int32_t>(old_lens[i])});
+        if (depths)
+          for (int32_t j = 0; j < nn[i]; ++j) pos.push_back(static_cast<int32_t>(old_lens[i]) + depths[row + j]);
+        else if (nn[i] > 0)
+          rc.push_back({row, static_cast<int32_t>(old_lens[i])});
         row += nn[i];
       }
-      st = run_rope_q(p, rc, total, g.n_layers, rotated->rope, rotated->q, rotated->q_out);
+      st = run_rope_q(p, rc, total, g.n_layers, rotated->rope, rotated->q, rotated->q_out, depths ? &pos : nullptr);
     }
   } catch (...) {
     st = out_of_memory();
@@ -823,6 +850,94 @@ cs_status append_impl(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t
   }
   for (int32_t i = 0; i < n; ++i) p->convs.find(convs[i])->len += n_new[i];
   return CS_OK;
+}
+
+// A tree for each conversation (n[i] tokens, at most kMaxDraft), their parents one after the other.
+cs_status check_trees(int32_t n_convs, const int32_t* n, const int32_t* parents) {
+  int64_t at = 0;
+  for (int32_t i = 0; i < n_convs; ++i) {
+    if (n[i] > cs::kMaxDraft)
+      return fail(CS_ERANGE, "a tree of " + std::to_string(n[i]) + " tokens: at most " + std::to_string(cs::kMaxDraft));
+    if (n[i] <= 0) continue;
+    if (!parents) return fail(CS_EINVAL, "null parents");
+    if (!cs::tree_ok(parents + at, n[i]))
+      return fail(CS_EINVAL, "a parent is neither -1 nor an earlier token of its tree (conversation " + std::to_string(i) + " of the batch)");
+    at += n[i];
+  }
+  return CS_OK;
+}
+
+// Batch entries [first, ..) whose descriptors and words fit one upload, laid out for a launch.
+struct SeenEntry {
+  int32_t slot, len, q_len;
+  int64_t q_row;
+  const int32_t* parents;   // null: the rows see every token
+};
+
+cs_status run_seen(cs_pool* p, const std::vector<SeenEntry>& entries, int32_t layer, const void* q, void* out) {
+  const cs::PoolGeom g = p->geom();
+  const size_t row_bytes = static_cast<size_t>(g.n_q_heads) * g.head_dim * 2;
+  for (size_t e0 = 0; e0 < entries.size();) {
+    std::vector<cs::ExtendConvDesc> convs;
+    std::vector<cs::SeenMask> masks;
+    std::vector<uint32_t> words;
+    int64_t rows = 0;
+    size_t e = e0;
+    for (; e < entries.size(); ++e) {
+      const SeenEntry& x = entries[e];
+      const size_t most = words.size() + (x.parents ? static_cast<size_t>(x.q_len) * (x.q_len / 32 + 2) : 0);
+      if (e > e0 && (convs.size() + 1) * (sizeof(cs::ExtendConvDesc) + sizeof(cs::SeenMask)) + most * 4 + 64 > kQuarter) break;
+      const int32_t off = static_cast<int32_t>(words.size());
+      const int32_t w = x.parents ? cs::tree_words(x.parents, x.q_len, x.len - x.q_len, words) : 0;
+      convs.push_back({x.slot, x.len, x.q_len, static_cast<int32_t>(x.q_row - entries[e0].q_row)});
+      masks.push_back({x.parents ? x.len - x.q_len : x.len, off, w, 0});
+      rows += x.q_len;
+    }
+    Blob b;
+    cs::SeenLaunch w;
+    b.push(convs.data(), convs.size());
+    w.masks_off = b.push(masks.data(), masks.size());
+    w.words_off = b.push(words.data(), words.size());
+    w.n_convs = static_cast<int>(convs.size());
+    w.rows = rows;
+    cs_status st = place_meta(p, b, &w.meta);
+    const size_t at = static_cast<size_t>(entries[e0].q_row) * row_bytes;
+    if (st == CS_OK)
+      st = timed_launch(p, CS_PROF_ATTN_FWD, "attention launch", [&] {
+        return cs::launch_seen_rows(g, layer, w, static_cast<const char*>(q) + at, static_cast<char*>(out) + at, p->stream);
+      });
+    if (st != CS_OK) return st;
+    e0 = e;
+  }
+  return CS_OK;
+}
+
+cs_status attend_seen(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t* q_lens, const int32_t* parents, bool tree,
+                      int32_t layer, const void* q, void* out, cs_stream stream) {
+  if (!p) return fail(CS_EINVAL, "null pool");
+  std::vector<const cs::Conv*> cv;
+  cs_status st = check_convs(p, n, convs, cv, tree);
+  if (st != CS_OK) return st;
+  if (n > 0 && !q_lens) return fail(CS_EINVAL, "null q_lens");
+  if (layer < 0 || layer >= p->desc.n_layers) return fail(CS_ERANGE, "layer out of range");
+  if (tree && (st = check_trees(n, q_lens, parents)) != CS_OK) return st;
+  int64_t rows = 0;
+  std::vector<SeenEntry> entries;
+  entries.reserve(static_cast<size_t>(n));
+  for (int32_t i = 0; i < n; ++i) {
+    if (q_lens[i] < 0) return fail(CS_EINVAL, "negative q_len");
+    if (tree && q_lens[i] > cv[i]->len)
+      return fail(CS_ESTATE, "q_len " + std::to_string(q_lens[i]) + " exceeds conversation length " + std::to_string(cv[i]->len));
+    if (q_lens[i] > 0)
+      entries.push_back({cs::ConvTable::slot_of(convs[i]), static_cast<int32_t>(cv[i]->len), q_lens[i], rows, tree ? parents + rows : nullptr});
+    rows += q_lens[i];
+  }
+  if (rows == 0) return CS_OK;
+  if (rows > INT32_MAX) return fail(CS_EINVAL, "too many query rows");
+  if (!q || !out) return fail(CS_EINVAL, "null q/out");
+  if ((st = ensure_device(p)) != CS_OK) return st;
+  if ((st = use_stream(p, as_stream(stream))) != CS_OK) return st;
+  return run_seen(p, entries, layer, q, out);
 }
 
 }  // namespace
@@ -1058,6 +1173,109 @@ cs_status cs_attn_prefill_turn1(cs_pool* p, int32_t n, const cs_conv* convs, con
 cs_status cs_attn_extend(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t* q_lens,
                          int32_t layer, const void* q, void* out, cs_stream stream) try {
   return attend(p, n, convs, q_lens, layer, q, out, stream, false);
+} CS_NO_THROW
+
+cs_status cs_attn_tree(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t* q_lens, const int32_t* parents, int32_t layer,
+                       const void* q, void* out, cs_stream stream) try {
+  return attend_seen(p, n, convs, q_lens, parents, true, layer, q, out, stream);
+} CS_NO_THROW
+
+cs_status cs_attn_cross(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t* q_lens, int32_t layer, const void* q, void* out,
+                        cs_stream stream) try {
+  return attend_seen(p, n, convs, q_lens, nullptr, false, layer, q, out, stream);
+} CS_NO_THROW
+
+cs_status cs_kv_append_tree(cs_pool* p, const cs_rope* rope, int32_t n, const cs_conv* convs, const int32_t* n_new,
+                            const int32_t* parents, const void* k, const void* v, const void* q, void* q_out, cs_stream stream) try {
+  if (!p) return fail(CS_EINVAL, "null pool");
+  RotatedAppend r;
+  cs_status st = rope_args(p->desc, rope, &r.rope);
+  if (st != CS_OK) return st;
+  if (q && !q_out) return fail(CS_EINVAL, "null q_out");
+  std::vector<const cs::Conv*> cv;
+  if ((st = check_convs(p, n, convs, cv)) != CS_OK) return st;
+  if (n > 0 && !n_new) return fail(CS_EINVAL, "null n_new");
+  for (int32_t i = 0; i < n; ++i)
+    if (n_new[i] < 0) return fail(CS_EINVAL, "negative token count");
+  if ((st = check_trees(n, n_new, parents)) != CS_OK) return st;
+  std::vector<int32_t> depths;
+  for (int32_t i = 0; i < n; ++i) {
+    const size_t at = depths.size();
+    depths.resize(at + static_cast<size_t>(n_new[i]));
+    cs::tree_depths(parents + at, n_new[i], depths.data() + at);
+  }
+  r.q = q;
+  r.q_out = q_out;
+  r.depths = depths.data();
+  return append_impl(p, n, convs, n_new, k, v, stream, nullptr, nullptr, &r);
+} CS_NO_THROW
+
+cs_status cs_kv_keep(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t* n_last, const int32_t* n_keep, const int32_t* keep,
+                     cs_stream stream) try {
+  if (!p) return fail(CS_EINVAL, "null pool");
+  std::vector<const cs::Conv*> cv;
+  cs_status st = check_convs(p, n, convs, cv);
+  if (st != CS_OK) return st;
+  if (n > 0 && (!n_last || !n_keep)) return fail(CS_EINVAL, "null n_last or n_keep");
+  const int32_t* at = keep;
+  for (int32_t i = 0; i < n; ++i) {
+    if (n_last[i] < 0 || n_keep[i] < 0 || n_keep[i] > n_last[i]) return fail(CS_EINVAL, "n_keep must be in 0 .. n_last");
+    if (n_last[i] > cv[i]->len)
+      return fail(CS_ESTATE, "n_last " + std::to_string(n_last[i]) + " exceeds conversation length " + std::to_string(cv[i]->len));
+    if (n_keep[i] == 0) continue;
+    if (!keep) return fail(CS_EINVAL, "null keep");
+    for (int32_t j = 0; j < n_keep[i]; ++j)
+      if (at[j] < 0 || at[j] >= n_last[i] || (j > 0 && at[j] <= at[j - 1]))
+        return fail(CS_EINVAL, "keep must be increasing indexes in 0 .. n_last - 1");
+    at += n_keep[i];
+  }
+  // What moves: from the first token that does not stay where it is. A last page that ends before its slots do is
+  // rewritten too, with zeros behind the end.
+  std::vector<cs::KeepConv> work;
+  std::vector<int32_t> src;
+  std::vector<int64_t> new_len(static_cast<size_t>(n));
+  std::vector<std::vector<int32_t>> dropped(static_cast<size_t>(n));
+  at = keep;
+  for (int32_t i = 0; i < n; ++i) {
+    const int64_t base = cv[i]->len - n_last[i];
+    int32_t j = 0;
+    while (j < n_keep[i] && at[j] == j) ++j;
+    const int64_t first = base + j, len = new_len[i] = base + n_keep[i];
+    if (len < cv[i]->len) {
+      const int64_t lp1 = cs::pages_for(len);
+      dropped[i].assign(cv[i]->pages.begin() + lp1, cv[i]->pages.end());
+      const int64_t lp0 = first / cs::kPage;
+      if (lp1 > lp0) {
+        work.push_back({cs::ConvTable::slot_of(convs[i]), static_cast<int32_t>(lp0), static_cast<int32_t>(lp1 - lp0),
+                        static_cast<int32_t>(first), static_cast<int32_t>(len), static_cast<int32_t>(src.size())});
+        for (int32_t x = j; x < n_keep[i]; ++x) src.push_back(static_cast<int32_t>(base + at[x]));
+      }
+    }
+    if (n_keep[i] > 0) at += n_keep[i];
+  }
+  if (!work.empty()) {
+    Blob b;
+    b.push(work.data(), work.size());
+    const size_t src_off = b.push(src.data(), src.size());
+    if (b.bytes.size() > kQuarter) return fail(CS_ENOMEM, "batch descriptor exceeds the metadata ring");
+    if ((st = ensure_device(p)) != CS_OK) return st;
+    hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+    CS_HIP(hipStreamIsCapturing(as_stream(stream), &cap), "hipStreamIsCapturing");
+    if (cap != hipStreamCaptureStatusNone) return fail(CS_ESTATE, "kv_keep cannot be captured: a replay would move the tokens again");
+    if ((st = use_stream(p, as_stream(stream))) != CS_OK) return st;
+    cs::Meta m;
+    if ((st = place_meta(p, b, &m)) != CS_OK) return st;
+    st = timed_launch(p, CS_PROF_APPEND, "keep launch",
+                      [&] { return cs::launch_keep(p->geom(), m, src_off, static_cast<int>(work.size()), p->stream); });
+    if (st != CS_OK) return st;
+  }
+  for (int32_t i = 0; i < n; ++i) {   // (allocates nothing)
+    cs::Conv* c = p->convs.find(convs[i]);
+    c->len = new_len[i];
+    c->pages.resize(c->pages.size() - dropped[i].size());
+    p->pages.release(dropped[i]);
+  }
+  return CS_OK;
 } CS_NO_THROW
 
 cs_status cs_attn_decode_batch(cs_pool* p, int32_t n, const cs_conv* convs, int32_t layer,

@@ -1,0 +1,35 @@
+// Host plans of the attention whose rows are not a conversation's last tokens in causal order: trees of
+// drafted tokens, and rows that see every token (an encoder's states). No HIP here.
+#pragma once
+
+#include <cstdint>
+#include <vector>
+
+#include "host_state.hpp"
+
+namespace cs {
+
+// What the rows of a batch entry see: every key before `clear`, and of the others those whose bits are set in the
+// row's words (none: `words` = 0, and clear = the conversation's length). Word w of a row stands for keys 32 (clear / 32
+// + w) .. + 31, bit b for key 32 (clear / 32 + w) + b: aligned to absolute keys, as the kernels meet them.
+struct SeenMask {
+  int32_t clear;
+  int32_t off;      // first word of the entry's rows, [q_len][words]
+  int32_t words;    // a row
+  int32_t rec;      // first record of the entry's work items (rows kernel)
+};
+
+// Tokens a tree may have (what bounds it: n^2 / 8 bytes of words).
+constexpr int kMaxDraft = 1024;
+
+// Whether parents[0 .. n) is a tree's: each -1 or an earlier token.
+bool tree_ok(const int32_t* parents, int32_t n);
+
+// Words of the rows of a tree of n tokens behind `prefix` cached ones, appended to `out`; returns the words a row. A
+// token sees what its parent sees, and itself.
+int32_t tree_words(const int32_t* parents, int32_t n, int64_t prefix, std::vector<uint32_t>& out);
+
+// Depth of each token (0: its parent is -1).
+void tree_depths(const int32_t* parents, int32_t n, int32_t* out);
+
+}  // namespace cs

@@ -6,6 +6,7 @@
 #include <cstring>
 
 #include "host/host_state.hpp"
+#include "host/seen.hpp"
 
 namespace cs {
 
@@ -75,17 +76,40 @@ struct RopeArgs {
 };
 
 // The append of 4-bit pools, and of both kinds with rotated keys (rope != nullptr). With q != nullptr the
-// launch also writes the rotated q [n_layers][src_rows][Hq][D] to q_out (may be q itself).
+// launch also writes the rotated q [n_layers][src_rows][Hq][D] to q_out (may be q itself). pos_off > 0: the positions that
+// tokens turn by are int32[n_chunks][16] there in meta, by token slot of the chunk's page; else they are the slots.
 hipError_t launch_append_as(const PoolGeom& g, const Meta& meta, int n_chunks, const AppendCarry& carry, const RopeArgs* rope,
-                            const void* k, const void* v, const void* q, void* q_out, int64_t src_rows, hipStream_t stream);
+                            const void* k, const void* v, const void* q, void* q_out, int64_t src_rows, size_t pos_off,
+                            hipStream_t stream);
 
-// Rotation of query rows q [n_layers][rows][Hq][D] into out (may be q): meta = RopeConv[n_convs].
+// Rotation of query rows q [n_layers][rows][Hq][D] into out (may be q): meta = RopeConv[n_convs], or with n_convs = 0
+// every row's position, int32[rows].
 struct RopeConv {
   int32_t row;   // first row of the conversation
   int32_t pos;   // its position
 };
 hipError_t launch_rope_q(const PoolGeom& g, const Meta& meta, int n_convs, int64_t rows, int n_layers, const RopeArgs& rope,
                          const void* q, void* out, hipStream_t stream);
+
+// Attention of rows that see what their words say (host/seen.hpp): meta = ExtendConvDesc[n_convs], SeenMask[n_convs] at
+// masks_off, the words at words_off. q, out: [rows][n_q_heads][head_dim].
+struct SeenLaunch {
+  Meta meta;
+  size_t masks_off = 0, words_off = 0;
+  int n_convs = 0;
+  int64_t rows = 0;
+};
+hipError_t launch_seen_rows(const PoolGeom& g, int layer, const SeenLaunch& w, const void* q, void* out, hipStream_t stream);
+
+// Keep of drafted tokens: meta = KeepConv[n_convs], then at src_off the source slots of the moved tokens.
+struct KeepConv {
+  int32_t slot;     // row of the page table
+  int32_t lp0, n_lp;   // logical pages that are rewritten
+  int32_t first;    // first token slot of the conversation that changes
+  int32_t len;      // its new length: slots [first, len) receive tokens, those behind them zeros
+  int32_t src;      // source slot of slot `first` + i: entry src + i
+};
+hipError_t launch_keep(const PoolGeom& g, const Meta& meta, size_t src_off, int n_convs, hipStream_t stream);
 
 // Workgroups that the queries of an append of n_chunks add to its launch.
 int64_t append_rope_groups(const PoolGeom& g, size_t n_chunks);

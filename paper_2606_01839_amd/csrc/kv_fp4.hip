@@ -44,6 +44,7 @@ __device__ __forceinline__ PageChunk load_chunk(ConstPtr<PageChunk> p) {
 // ---------------------------------------------------------------------------------------------
 struct AppendArgs {
   const void* meta;
+  uint32_t pos_off;   // positions of the tokens in meta; 0: their slots
   int n_chunks;
   int n_layers, n_kv_heads, n_q_heads;
   int kv_blocks;   // grid rows of the K and V; the queries' follow
@@ -111,7 +112,8 @@ __global__ __launch_bounds__(256) void kv_append_as_kernel(LaunchMeta, RopeArgs 
     int pos = -1;
 #pragma unroll
     for (int i = 0; i < CH; ++i)
-      if (row / kPageTokens == i && have[i] && t >= c[i].t0 && t < c[i].t1) pos = c[i].lpage * kPageTokens + t;
+      if (row / kPageTokens == i && have[i] && t >= c[i].t0 && t < c[i].t1)
+        pos = a.pos_off ? meta_at<int32_t>(a.meta, a.pos_off)[(blockIdx.x * CH + i) * kPageTokens + t] : c[i].lpage * kPageTokens + t;
     return pos;
   };
   // 16 bytes of row t of a chunk: [layer][row][head][D] + 8 ch
@@ -277,6 +279,7 @@ __global__ __launch_bounds__(256) void rope_q_kernel(LaunchMeta, RopeArgs rope, 
   rope_table<D>(tab, kPageTokens, rope, 4, [&](int t) {
     const int64_t row = row0 + t;
     if (row >= rows) return -1;
+    if (n_convs == 0) return static_cast<int>(meta_at<int32_t>(meta, 0)[row]);
     int lo = 0, hi = n_convs - 1;   // the last conversation that starts at or before the row
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
@@ -543,9 +546,11 @@ static hipError_t by_dim(int D, F&& f) {
 static int head_waves(int n_kv_heads) { return n_kv_heads % 4 == 0 ? 4 : (n_kv_heads % 2 == 0 ? 2 : 1); }
 
 hipError_t launch_append_as(const PoolGeom& g, const Meta& meta, int n_chunks, const AppendCarry& carry, const RopeArgs* rope,
-                            const void* k, const void* v, const void* q, void* q_out, int64_t src_rows, hipStream_t stream) {
+                            const void* k, const void* v, const void* q, void* q_out, int64_t src_rows, size_t pos_off,
+                            hipStream_t stream) {
   if (n_chunks == 0) return hipSuccess;
   if (!meta.ok() || meta.bytes < n_chunks * sizeof(PageChunk)) return hipErrorInvalidValue;
+  if (pos_off > 0 && (rope == nullptr || meta.bytes < pos_off + n_chunks * kPageTokens * sizeof(int32_t))) return hipErrorInvalidValue;
   if (carry.bytes > 0 && (meta.dev != nullptr || carry.dst == nullptr || carry.off % 16 || carry.bytes % 16 ||
                           carry.off + carry.bytes > meta.bytes))
     return hipErrorInvalidValue;
@@ -556,6 +561,7 @@ hipError_t launch_append_as(const PoolGeom& g, const Meta& meta, int n_chunks, c
   const int waves = head_waves(g.n_kv_heads);
   AppendArgs a{};
   a.meta = meta.dev;
+  a.pos_off = static_cast<uint32_t>(pos_off);
   a.n_chunks = n_chunks;
   a.n_layers = g.n_layers;
   a.n_kv_heads = g.n_kv_heads;
@@ -594,7 +600,8 @@ int rope_q_layers(const PoolGeom& g) { return std::max(1, 65535 / ((g.n_q_heads 
 hipError_t launch_rope_q(const PoolGeom& g, const Meta& meta, int n_convs, int64_t rows, int n_layers, const RopeArgs& rope,
                          const void* q, void* out, hipStream_t stream) {
   if (rows == 0 || n_layers == 0) return hipSuccess;
-  if (n_convs < 1 || !meta.ok() || meta.bytes < n_convs * sizeof(RopeConv)) return hipErrorInvalidValue;
+  if (n_convs < 0 || !meta.ok() || meta.bytes < (n_convs > 0 ? n_convs * sizeof(RopeConv) : rows * sizeof(int32_t)))
+    return hipErrorInvalidValue;
   if (rope.pairs < 8 || rope.pairs % 8 || 2 * rope.pairs > g.head_dim) return hipErrorInvalidValue;
   LaunchMeta m;
   fill_meta(meta, &m);
