@@ -867,49 +867,90 @@ cs_status check_trees(int32_t n_convs, const int32_t* n, const int32_t* parents)
   return CS_OK;
 }
 
-// Batch entries [first, ..) whose descriptors and words fit one upload, laid out for a launch.
+// Rows of one batch entry of a tree or cross attention.
 struct SeenEntry {
   int32_t slot, len, q_len;
   int64_t q_row;
-  const int32_t* parents;   // null: the rows see every token
+  const int32_t* parents;   // null: the rows see every key
 };
 
-cs_status run_seen(cs_pool* p, const std::vector<SeenEntry>& entries, int32_t layer, const void* q, void* out) {
+// Entries without a parent list may be cut into pieces of this many rows, so that any number of tiles is several uploads.
+constexpr int32_t kSeenRows = 32768;
+
+cs_status run_seen_tiles(cs_pool* p, const std::vector<SeenEntry>& entries, bool all, int32_t layer, const void* q, void* out) {
   const cs::PoolGeom g = p->geom();
   const size_t row_bytes = static_cast<size_t>(g.n_q_heads) * g.head_dim * 2;
+  const int tile = cs::extend_query_tile(g.n_q_heads / g.n_kv_heads);
   for (size_t e0 = 0; e0 < entries.size();) {
-    std::vector<cs::ExtendConvDesc> convs;
+    // as many entries as one upload holds
+    std::vector<int32_t> slots, q_lens;
+    std::vector<int64_t> lens;
     std::vector<cs::SeenMask> masks;
     std::vector<uint32_t> words;
-    int64_t rows = 0;
-    size_t e = e0;
+    size_t bytes = kMaxCutBytes + 4 * kAlign, e = e0;
+    const int64_t row0 = entries[e0].q_row;
     for (; e < entries.size(); ++e) {
       const SeenEntry& x = entries[e];
-      const size_t most = words.size() + (x.parents ? static_cast<size_t>(x.q_len) * (x.q_len / 32 + 2) : 0);
-      if (e > e0 && (convs.size() + 1) * (sizeof(cs::ExtendConvDesc) + sizeof(cs::SeenMask)) + most * 4 + 64 > kQuarter) break;
+      bytes += sizeof(cs::ExtendConvDesc) + sizeof(cs::SeenMask) + (x.q_len + tile - 1) / tile * sizeof(cs::ExtendTile);
+      if (x.parents) bytes += static_cast<size_t>(x.q_len) * (x.q_len / 32 + 2) * 4;
+      // (rows of a launch are counted from its first entry's)
+      if (e > e0 && (bytes > kQuarter || x.q_row + x.q_len - row0 > INT32_MAX)) break;
       const int32_t off = static_cast<int32_t>(words.size());
       const int32_t w = x.parents ? cs::tree_words(x.parents, x.q_len, x.len - x.q_len, words) : 0;
-      convs.push_back({x.slot, x.len, x.q_len, static_cast<int32_t>(x.q_row - entries[e0].q_row)});
+      slots.push_back(x.slot);
+      lens.push_back(x.len);
+      q_lens.push_back(x.q_len);
       masks.push_back({x.parents ? x.len - x.q_len : x.len, off, w, 0});
-      rows += x.q_len;
     }
+    cs::ExtendPlan plan = cs::plan_extend(slots, lens, q_lens, tile, all);
+    for (size_t i = e0; i < e; ++i) plan.convs[i - e0].q_row = static_cast<int32_t>(entries[i].q_row - row0);
+    cs::split_extend(plan, g.n_kv_heads, cs::kCus, kExtendRecords);
     Blob b;
-    cs::SeenLaunch w;
-    b.push(convs.data(), convs.size());
-    w.masks_off = b.push(masks.data(), masks.size());
-    w.words_off = b.push(words.data(), words.size());
-    w.n_convs = static_cast<int>(convs.size());
-    w.rows = rows;
+    size_t off = 0;
+    cs::ExtendLaunch w = push_extend(plan, 0, plan.tiles.size(), &b, &off);
+    w.masks_off = b.push(masks.data(), masks.size()) - off;
+    w.words_off = b.push(words.data(), words.size()) - off;
     cs_status st = place_meta(p, b, &w.meta);
-    const size_t at = static_cast<size_t>(entries[e0].q_row) * row_bytes;
+    const char* qe = static_cast<const char*>(q) + row0 * row_bytes;
+    char* oe = static_cast<char*>(out) + row0 * row_bytes;
     if (st == CS_OK)
-      st = timed_launch(p, CS_PROF_ATTN_FWD, "attention launch", [&] {
-        return cs::launch_seen_rows(g, layer, w, static_cast<const char*>(q) + at, static_cast<char*>(out) + at, p->stream);
-      });
+      st = timed_launch(p, CS_PROF_ATTN_FWD, "attention launch",
+                        [&] { return cs::launch_seen_tiles(g, layer, w, qe, oe, p->ext_parts(), p->stream); });
+    if (st == CS_OK && w.n_merges > 0)
+      st = timed_launch(p, CS_PROF_ATTN_FWD, "attention merge launch",
+                        [&] { return cs::launch_extend_merge(g, 1, w, oe, p->ext_parts(), p->stream); });
     if (st != CS_OK) return st;
     e0 = e;
   }
   return CS_OK;
+}
+
+cs_status run_seen(cs_pool* p, const std::vector<SeenEntry>& entries, bool all, int32_t layer, const void* q, void* out) {
+  std::vector<SeenEntry> tiles;
+  std::vector<cs::SeenEmpty> empty;
+  for (const SeenEntry& x : entries) {
+    if (x.len == 0) {
+      empty.push_back({x.q_row, x.q_len});
+    } else if (x.parents) {
+      tiles.push_back(x);
+    } else {
+      for (int32_t r = 0; r < x.q_len; r += std::min(x.q_len - r, kSeenRows))
+        tiles.push_back({x.slot, x.len, std::min(x.q_len - r, kSeenRows), x.q_row + r, nullptr});
+    }
+  }
+  constexpr size_t kEmpty = kQuarter / sizeof(cs::SeenEmpty) - 1;
+  for (size_t i = 0; i < empty.size(); i += kEmpty) {
+    Blob b;
+    const size_t n = std::min(kEmpty, empty.size() - i);
+    b.push(empty.data() + i, n);
+    cs::Meta m;
+    cs_status st = place_meta(p, b, &m);
+    if (st == CS_OK)
+      st = timed_launch(p, CS_PROF_ATTN_FWD, "attention launch",
+                        [&] { return cs::launch_seen_empty(p->geom(), m, static_cast<int>(n), out, p->stream); });
+    if (st != CS_OK) return st;
+  }
+  return run_seen_tiles(p, tiles, all, layer, q, out);
 }
 
 cs_status attend_seen(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t* q_lens, const int32_t* parents, bool tree,
@@ -937,7 +978,7 @@ cs_status attend_seen(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t
   if (!q || !out) return fail(CS_EINVAL, "null q/out");
   if ((st = ensure_device(p)) != CS_OK) return st;
   if ((st = use_stream(p, as_stream(stream))) != CS_OK) return st;
-  return run_seen(p, entries, layer, q, out);
+  return run_seen(p, entries, !tree, layer, q, out);
 }
 
 }  // namespace

@@ -151,16 +151,17 @@ DecodePlan plan_decode_rounds(const std::vector<int32_t>& slots, const std::vect
 }
 
 ExtendPlan plan_extend(const std::vector<int32_t>& slots, const std::vector<int64_t>& lens,
-                       const std::vector<int32_t>& q_lens, int32_t q_tile) {
+                       const std::vector<int32_t>& q_lens, int32_t q_tile, bool all) {
   ExtendPlan plan;
   plan.q_tile = q_tile;
+  plan.all = all;
   int32_t row = 0;
   std::vector<std::pair<int64_t, ExtendTile>> work;
   for (size_t i = 0; i < lens.size(); ++i) {
     plan.convs.push_back({slots[i], static_cast<int32_t>(lens[i]), q_lens[i], row});
     row += q_lens[i];
     for (int32_t q0 = 0; q0 < q_lens[i]; q0 += q_tile) {
-      int64_t keys = lens[i] - q_lens[i] + std::min(q_lens[i], q0 + q_tile);
+      int64_t keys = plan.seen(plan.convs.back(), q0);
       work.push_back({keys, {static_cast<int32_t>(i), q0, 0, -1}});
     }
   }
@@ -231,7 +232,7 @@ void split_extend(ExtendPlan& plan, int32_t n_kv_heads, int32_t n_cus, int32_t m
   int64_t total = 0;
   for (int i = 0; i < n; ++i) {
     const ExtendConvDesc& c = plan.convs[static_cast<size_t>(plan.tiles[i].conv)];
-    const int32_t seen = c.len - c.q_len + std::min(c.q_len, plan.tiles[i].q0 + plan.q_tile);
+    const int32_t seen = plan.seen(c, plan.tiles[i].q0);
     keys[i] = (seen + kExtendKeyTile - 1) / kExtendKeyTile;
     total += keys[i];
   }

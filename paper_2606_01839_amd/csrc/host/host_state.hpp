@@ -178,10 +178,15 @@ struct ExtendPlan {
   int32_t piece = 0;    // key tiles per piece
   int32_t n_parts = 0;  // pieces (per kv head)
   std::vector<ExtendMerge> merges;
+  bool all = false;     // every query sees every key (queries need not be the conversation's last tokens)
+  // Keys that the tile from query q0 on sees.
+  int32_t seen(const ExtendConvDesc& c, int32_t q0) const {
+    return all || q0 + q_tile >= c.q_len ? c.len : c.len - c.q_len + q0 + q_tile;
+  }
 };
 
 ExtendPlan plan_extend(const std::vector<int32_t>& slots, const std::vector<int64_t>& lens,
-                       const std::vector<int32_t>& q_lens, int32_t q_tile);
+                       const std::vector<int32_t>& q_lens, int32_t q_tile, bool all = false);
 
 // Cut the keys of a launch's tiles into pieces where the tiles alone would leave CUs idle; at most
 // max_records pieces over all kv heads. Changes nothing where the tiles fill the chip. Pieces are

@@ -91,16 +91,6 @@ struct RopeConv {
 hipError_t launch_rope_q(const PoolGeom& g, const Meta& meta, int n_convs, int64_t rows, int n_layers, const RopeArgs& rope,
                          const void* q, void* out, hipStream_t stream);
 
-// Attention of rows that see what their words say (host/seen.hpp): meta = ExtendConvDesc[n_convs], SeenMask[n_convs] at
-// masks_off, the words at words_off. q, out: [rows][n_q_heads][head_dim].
-struct SeenLaunch {
-  Meta meta;
-  size_t masks_off = 0, words_off = 0;
-  int n_convs = 0;
-  int64_t rows = 0;
-};
-hipError_t launch_seen_rows(const PoolGeom& g, int layer, const SeenLaunch& w, const void* q, void* out, hipStream_t stream);
-
 // Keep of drafted tokens: meta = KeepConv[n_convs], then at src_off the source slots of the moved tokens.
 struct KeepConv {
   int32_t slot;     // row of the page table
@@ -182,6 +172,7 @@ struct ExtendLaunch {
   int piece = 0, n_parts = 0;
   bool chained = false;  // some tiles hold their pieces (ExtendTile::k0 < 0)
   int64_t q_rows = 0;  // query rows of a layer
+  size_t masks_off = 0, words_off = 0;   // launch_seen_tiles: SeenMask[..] of the conversations, and their words
 };
 
 // One layer of a mixed step in one launch: the extend tiles of the layer and its decode split
@@ -203,5 +194,17 @@ hipError_t launch_extend(const PoolGeom& g, int layer, int n_layers, const Exten
                          float* parts, hipStream_t stream);
 hipError_t launch_extend_merge(const PoolGeom& g, int n_layers, const ExtendLaunch& e, void* out, float* parts,
                                hipStream_t stream);
+
+// Attention of rows that see what their words say (host/seen.hpp), in tiles as launch_extend's; pieces are joined by
+// launch_extend_merge.
+hipError_t launch_seen_tiles(const PoolGeom& g, int layer, const ExtendLaunch& e, const void* q, void* out, float* parts,
+                             hipStream_t stream);
+
+// Rows of zeros: those of conversations without a key. meta: SeenEmpty[n].
+struct SeenEmpty {
+  int64_t row;   // first row
+  int64_t n;
+};
+hipError_t launch_seen_empty(const PoolGeom& g, const Meta& meta, int n, void* out, hipStream_t stream);
 
 }  // namespace cs
