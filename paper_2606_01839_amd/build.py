@@ -18,7 +18,7 @@ OUT = os.path.join(PKG, "libconserve_attn.so")
 BUILD = os.path.join(PKG, "_build")
 
 SOURCES = ["host/host_state.cpp", "host/sched.cpp", "host/seen.cpp", "capi.cpp", "sched_capi.cpp", "kv_move.hip", "kv_fp4.hip", "kv_keep.hip",
-           "decode.hip", "attn_fwd.hip", "seen_tile.hip", "probe.hip"]
+           "decode.hip", "attn_fwd.hip", "seen_rows.hip", "seen_tile.hip", "probe.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

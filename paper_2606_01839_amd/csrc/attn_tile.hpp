@@ -105,9 +105,6 @@ __device__ __forceinline__ void lds_wait() { asm volatile("s_waitcnt lgkmcnt(0)"
 __device__ __forceinline__ void bare_barrier() { asm volatile("s_barrier" ::: "memory"); }
 __device__ __forceinline__ void lds_wait_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// Bits 15 and 31: the bf16 value in the low, high half of w is an infinity or NaN.
-__device__ __forceinline__ uint32_t not_finite(uint32_t w) { return ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }
-
 // One (tile or piece, kv head) workgroup (`block` = its index in the layer's grid, `dl` = its layer
 // counted from a.layer).
 //

@@ -875,7 +875,7 @@ struct SeenEntry {
 };
 
 // Entries without a parent list may be cut into pieces of this many rows, so that any number of tiles is several uploads.
-constexpr int32_t kSeenRows = 32768;
+constexpr int32_t kSeenCut = 32768;
 
 cs_status run_seen_tiles(cs_pool* p, const std::vector<SeenEntry>& entries, bool all, int32_t layer, const void* q, void* out) {
   const cs::PoolGeom g = p->geom();
@@ -925,17 +925,112 @@ cs_status run_seen_tiles(cs_pool* p, const std::vector<SeenEntry>& entries, bool
   return CS_OK;
 }
 
+// Entries of few rows. One too long for the records goes to `tiles`.
+cs_status run_seen_rows(cs_pool* p, const std::vector<SeenEntry>& entries, int32_t layer, const void* q, void* out,
+                        std::vector<SeenEntry>* tiles) {
+  const cs::PoolGeom g = p->geom();
+  const size_t row_bytes = static_cast<size_t>(g.n_q_heads) * g.head_dim * 2;
+  const int group = g.n_q_heads / g.n_kv_heads;
+  const size_t room = (p->lay.ring - p->lay.ext_parts) / 4;   // floats of records
+  for (size_t e0 = 0; e0 < entries.size();) {
+    // As many entries as one upload holds and whose records have room.
+    size_t e = e0, bytes = 4 * kAlign;
+    const int64_t row0 = entries[e0].q_row;
+    for (; e < entries.size(); ++e) {
+      const SeenEntry& x = entries[e];
+      bytes += sizeof(cs::ExtendConvDesc) + sizeof(cs::SeenMask) + sizeof(int32_t) +
+               (x.len / (cs::kDecodeSubSplits * 32) + 1) * sizeof(cs::SeenItem);
+      if (x.parents) bytes += static_cast<size_t>(x.q_len) * (x.q_len / 32 + 2) * 4;
+      if (e > e0 && (bytes > kQuarter || x.q_row + x.q_len - row0 > INT32_MAX)) break;
+    }
+    cs::DecodePlan plan;
+    int rows = 0;
+    cs::SeenLaunch w;
+    std::vector<int32_t> slots;
+    std::vector<int64_t> lens;
+    for (;; e = e0 + (e - e0) / 2) {
+      slots.clear();
+      lens.clear();
+      rows = 0;
+      for (size_t i = e0; i < e; ++i) {
+        slots.push_back(entries[i].slot);
+        lens.push_back(entries[i].len);
+        rows = std::max(rows, entries[i].q_len * group);
+      }
+      w.blocks = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+      if (e == e0) break;
+      plan = plan_decode_batch(p, slots, lens);
+      size_t records = 0;
+      for (const auto& c : plan.convs) records += c.n_splits > 1 ? c.n_splits : 0;
+      if (records * g.n_kv_heads * 16 * w.blocks * cs::partial_floats(g.head_dim) <= room &&
+          plan.n_items * sizeof(cs::SeenItem) <= kQuarter / 2) break;
+    }
+    if (e == e0) {
+      tiles->push_back(entries[e0++]);
+      continue;
+    }
+    std::vector<cs::ExtendConvDesc> convs;
+    std::vector<cs::SeenMask> masks;
+    std::vector<uint32_t> words;
+    std::vector<int32_t> merges, conv_of(static_cast<size_t>(plan.n_items));
+    int32_t rec = 0;
+    for (size_t i = e0; i < e; ++i) {
+      const SeenEntry& x = entries[i];
+      const cs::DecodeConvDesc& d = plan.convs[i - e0];
+      const int32_t off = static_cast<int32_t>(words.size()), c = static_cast<int32_t>(i - e0);
+      const int32_t n = x.parents ? cs::tree_words(x.parents, x.q_len, x.len - x.q_len, words) : 0;
+      convs.push_back({x.slot, x.len, x.q_len, static_cast<int32_t>(x.q_row - row0)});
+      masks.push_back({x.parents ? x.len - x.q_len : x.len, off, n, d.n_splits > 1 ? rec : -1});
+      if (d.n_splits > 1) {
+        rec += d.n_splits;
+        merges.push_back(c);
+        w.merge_rows = std::max(w.merge_rows, x.q_len * group);
+      }
+      std::fill_n(conv_of.begin() + d.item_start, d.n_splits, c);
+    }
+    std::vector<cs::SeenItem> items;
+    items.reserve(plan.order.size());
+    for (const int32_t i : plan.order) {
+      const int32_t c = conv_of[static_cast<size_t>(i)];
+      items.push_back({c, (i - plan.convs[static_cast<size_t>(c)].item_start) * cs::kDecodeSubSplits * plan.split_tokens});
+    }
+    Blob b;
+    b.push(convs.data(), convs.size());
+    w.masks_off = b.push(masks.data(), masks.size());
+    w.items_off = b.push(items.data(), items.size());
+    w.merges_off = b.push(merges.data(), merges.size());
+    w.words_off = b.push(words.data(), words.size());
+    w.n_items = plan.n_items;
+    w.n_merges = static_cast<int>(merges.size());
+    w.split = plan.split_tokens;
+    cs_status st = place_meta(p, b, &w.meta);
+    const char* qe = static_cast<const char*>(q) + row0 * row_bytes;
+    char* oe = static_cast<char*>(out) + row0 * row_bytes;
+    if (st == CS_OK)
+      st = timed_launch(p, CS_PROF_ATTN_FWD, "attention launch",
+                        [&] { return cs::launch_seen_rows(g, layer, w, qe, oe, p->ext_parts(), p->stream); });
+    if (st == CS_OK && w.n_merges > 0)
+      st = timed_launch(p, CS_PROF_ATTN_FWD, "attention merge launch",
+                        [&] { return cs::launch_seen_rows_merge(g, w, oe, p->ext_parts(), p->stream); });
+    if (st != CS_OK) return st;
+    e0 = e;
+  }
+  return CS_OK;
+}
+
 cs_status run_seen(cs_pool* p, const std::vector<SeenEntry>& entries, bool all, int32_t layer, const void* q, void* out) {
-  std::vector<SeenEntry> tiles;
+  std::vector<SeenEntry> rows, tiles;
   std::vector<cs::SeenEmpty> empty;
   for (const SeenEntry& x : entries) {
     if (x.len == 0) {
       empty.push_back({x.q_row, x.q_len});
+    } else if (static_cast<int64_t>(x.q_len) * (p->desc.n_q_heads / p->desc.n_kv_heads) <= cs::kSeenRows) {
+      rows.push_back(x);
     } else if (x.parents) {
       tiles.push_back(x);
     } else {
-      for (int32_t r = 0; r < x.q_len; r += std::min(x.q_len - r, kSeenRows))
-        tiles.push_back({x.slot, x.len, std::min(x.q_len - r, kSeenRows), x.q_row + r, nullptr});
+      for (int32_t r = 0; r < x.q_len; r += std::min(x.q_len - r, kSeenCut))
+        tiles.push_back({x.slot, x.len, std::min(x.q_len - r, kSeenCut), x.q_row + r, nullptr});
     }
   }
   constexpr size_t kEmpty = kQuarter / sizeof(cs::SeenEmpty) - 1;
@@ -950,7 +1045,8 @@ cs_status run_seen(cs_pool* p, const std::vector<SeenEntry>& entries, bool all, 
                         [&] { return cs::launch_seen_empty(p->geom(), m, static_cast<int>(n), out, p->stream); });
     if (st != CS_OK) return st;
   }
-  return run_seen_tiles(p, tiles, all, layer, q, out);
+  const cs_status st = run_seen_rows(p, rows, layer, q, out, &tiles);
+  return st == CS_OK ? run_seen_tiles(p, tiles, all, layer, q, out) : st;
 }
 
 cs_status attend_seen(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t* q_lens, const int32_t* parents, bool tree,

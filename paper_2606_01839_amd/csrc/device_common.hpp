@@ -82,6 +82,9 @@ __device__ __forceinline__ uint32_t mask_bf16x2(uint32_t w, bool keep_lo, bool k
   return w & ((keep_lo ? 0x0000FFFFu : 0u) | (keep_hi ? 0xFFFF0000u : 0u));
 }
 
+// Bits 15 and 31: the bf16 value in the low, high half of w is an infinity or NaN.
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) { return ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }
+
 // Cross-lane exchange within a wave64 (ds_bpermute); lane ^ mask.
 __device__ __forceinline__ float xor_shfl(float v, int mask) {
   int lane = __lane_id();

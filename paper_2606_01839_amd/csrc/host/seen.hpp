@@ -19,6 +19,12 @@ struct SeenMask {
   int32_t rec;      // first record of the entry's work items (rows kernel)
 };
 
+// A work item of the rows kernel: keys [k0, k0 + kDecodeSubSplits x split) of a batch entry.
+struct SeenItem {
+  int32_t conv;
+  int32_t k0;
+};
+
 // Tokens a tree may have (what bounds it: n^2 / 8 bytes of words).
 constexpr int kMaxDraft = 1024;
 

@@ -195,7 +195,23 @@ hipError_t launch_extend(const PoolGeom& g, int layer, int n_layers, const Exten
 hipError_t launch_extend_merge(const PoolGeom& g, int n_layers, const ExtendLaunch& e, void* out, float* parts,
                                hipStream_t stream);
 
-// Attention of rows that see what their words say (host/seen.hpp), in tiles as launch_extend's; pieces are joined by
+// Attention of rows that see what their words say (host/seen.hpp), at most kSeenRows rows (query tokens x query heads of a kv head) an entry: meta = ExtendConvDesc[..], and SeenMask[..],
+// the words, SeenItem[n_items] in launch order and int32[n_merges] (entries of several items) at their offsets. Records of
+// the items of entries with several: SeenMask::rec + item, [kv head][16 blocks rows] of partial_floats each.
+constexpr int kSeenRows = 64;
+struct SeenLaunch {
+  Meta meta;
+  size_t masks_off = 0, words_off = 0, items_off = 0, merges_off = 0;
+  int n_items = 0, n_merges = 0;
+  int merge_rows = 0;   // the most rows of an entry of several items
+  int blocks = 1;       // blocks of 16 rows: 1, 2 or 4
+  int split = 0;        // keys per wave
+};
+hipError_t launch_seen_rows(const PoolGeom& g, int layer, const SeenLaunch& w, const void* q, void* out, float* parts,
+                            hipStream_t stream);
+hipError_t launch_seen_rows_merge(const PoolGeom& g, const SeenLaunch& w, void* out, float* parts, hipStream_t stream);
+
+// The same for any number of rows, in tiles as launch_extend's; pieces are joined by
 // launch_extend_merge.
 hipError_t launch_seen_tiles(const PoolGeom& g, int layer, const ExtendLaunch& e, const void* q, void* out, float* parts,
                              hipStream_t stream);
