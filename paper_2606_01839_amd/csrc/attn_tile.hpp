@@ -77,9 +77,6 @@ constexpr float kFarScore = 0x1p23f;
 // bank groups (rocprofv3 SQ_LDS_BANK_CONFLICT counts about 100 cycles a wave, those of the output rows
 // at the end), while every copy instruction still writes 1 KiB of consecutive LDS bytes.
 // ------------------------------------------------------------------------------------------------
-__device__ __forceinline__ uint32_t lds_u32(const void* p) {
-  return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void*)p));
-}
 // Copy 16 bytes per lane from global memory (wave-uniform base + per-lane byte offset) straight
 // into LDS: lane l writes LDS bytes lds + 16 l .. +15 (global_load_lds_dwordx4, destination base in
 // M0). The copy is tracked by the vector-memory counter only; M0 is saved and restored around it.

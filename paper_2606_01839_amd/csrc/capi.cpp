@@ -957,9 +957,9 @@ cs_status run_seen_rows(cs_pool* p, const std::vector<SeenEntry>& entries, int32
         lens.push_back(entries[i].len);
         rows = std::max(rows, entries[i].q_len * group);
       }
-      w.blocks = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+      w.blocks = (rows + 15) / 16;
       if (e == e0) break;
-      plan = plan_decode_batch(p, slots, lens);
+      plan = cs::decode_plan_of(slots, lens, cs::rows_split(lens, g.n_kv_heads, cs::kCus));
       size_t records = 0;
       for (const auto& c : plan.convs) records += c.n_splits > 1 ? c.n_splits : 0;
       if (records * g.n_kv_heads * 16 * w.blocks * cs::partial_floats(g.head_dim) <= room &&
@@ -985,6 +985,7 @@ cs_status run_seen_rows(cs_pool* p, const std::vector<SeenEntry>& entries, int32
         rec += d.n_splits;
         merges.push_back(c);
         w.merge_rows = std::max(w.merge_rows, x.q_len * group);
+        w.merge_items = std::max(w.merge_items, d.n_splits);
       }
       std::fill_n(conv_of.begin() + d.item_start, d.n_splits, c);
     }

@@ -85,7 +85,7 @@ void ConvTable::destroy(int32_t handle, PagePool& pool) {
 }
 
 // The items and launch order of a plan with splits of `split` keys.
-static DecodePlan decode_plan_of(const std::vector<int32_t>& slots, const std::vector<int64_t>& lens, int32_t split) {
+DecodePlan decode_plan_of(const std::vector<int32_t>& slots, const std::vector<int64_t>& lens, int32_t split) {
   DecodePlan plan;
   plan.split_tokens = split;
   const int64_t item_keys = static_cast<int64_t>(kDecodeSubSplits) * split;

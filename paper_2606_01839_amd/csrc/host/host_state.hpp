@@ -136,6 +136,9 @@ DecodePlan plan_decode_filling(const std::vector<int32_t>& slots, const std::vec
 DecodePlan plan_decode_rounds(const std::vector<int32_t>& slots, const std::vector<int64_t>& lens,
                               int32_t n_kv_heads, int64_t target_items, int32_t n_cus);
 
+// Items and launch order of splits of `split` keys.
+DecodePlan decode_plan_of(const std::vector<int32_t>& slots, const std::vector<int64_t>& lens, int32_t split);
+
 // Extend / prefill: queries are the last q_len tokens of each conversation, cut into tiles of q_tile
 // query tokens; one tile = (conversation, query block) x one kv head.
 struct ExtendConvDesc {

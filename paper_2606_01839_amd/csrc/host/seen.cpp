@@ -4,6 +4,22 @@
 
 namespace cs {
 
+int32_t rows_split(const std::vector<int64_t>& lens, int32_t n_kv_heads, int32_t n_cus) {
+  int64_t keys = 0;
+  for (const int64_t n : lens) keys += n;
+  const int64_t share = keys * n_kv_heads / n_cus;   // of a CU
+  for (const int64_t most : {2 * n_cus, 3 * n_cus, 4 * n_cus}) {   // twice the workgroups
+    for (int32_t split = 32; split <= 1024; split += 32) {
+      const int64_t item = static_cast<int64_t>(kDecodeSubSplits) * split;
+      if (item > std::max<int64_t>(2 * share, 1024)) break;
+      int64_t items = 0;
+      for (const int64_t n : lens) items += (n + item - 1) / item;
+      if (2 * items * n_kv_heads <= most) return split;
+    }
+  }
+  return 1024;
+}
+
 bool tree_ok(const int32_t* parents, int32_t n) {
   for (int32_t i = 0; i < n; ++i)
     if (parents[i] < -1 || parents[i] >= i) return false;

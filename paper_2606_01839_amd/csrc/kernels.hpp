@@ -203,8 +203,8 @@ struct SeenLaunch {
   Meta meta;
   size_t masks_off = 0, words_off = 0, items_off = 0, merges_off = 0;
   int n_items = 0, n_merges = 0;
-  int merge_rows = 0;   // the most rows of an entry of several items
-  int blocks = 1;       // blocks of 16 rows: 1, 2 or 4
+  int merge_rows = 0, merge_items = 0;   // the most rows, and items, of an entry of several items
+  int blocks = 1;       // blocks of 16 rows: 1 to 4
   int split = 0;        // keys per wave
 };
 hipError_t launch_seen_rows(const PoolGeom& g, int layer, const SeenLaunch& w, const void* q, void* out, float* parts,

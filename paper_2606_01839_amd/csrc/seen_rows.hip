@@ -66,7 +66,7 @@ __device__ __forceinline__ void rows_body(const RowsArgs& a) {
   constexpr int KS = D / 32, DT = D / 16, R = partial_floats(D);
   constexpr bool QLDS = NB > 2;             // queries in LDS instead of registers
   constexpr int QW = FP4 ? 5 : KS;          // 16-byte words of a lane's query operand, a block
-  constexpr int NX = NB > 1 ? 2 : 1;        // exchange buffers
+  constexpr int NX = NB > 1 ? 2 : 1;        // blocks the waves exchange at a time
   __shared__ __attribute__((aligned(16))) float xch[NX][kRowWaves][16][R];
   __shared__ uint4 q_lds[QLDS ? NB : 1][QLDS ? QW : 1][64];
 
@@ -210,6 +210,20 @@ __device__ __forceinline__ void rows_body(const RowsArgs& a) {
   auto step = [&](const Page& pa, const Page& pb, const int j) {
     const int k = k_begin + kPageTokens * j;
     const bool partly = k + 2 * kPageTokens > mk.clear;
+    uint32_t seen_w[NB];   // of the lane's rows, for the 32 keys
+    if (partly) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        if (mk.words > 0) {
+          const int w = (k >> 5) - (mk.clear >> 5), i = (16 * nb + c) >> a.group_log2;
+          const uint32_t* words = (const uint32_t*)meta_at<uint32_t>(a.meta, a.words_off) + mk.off;
+          seen_w[nb] = w < mk.words ? words[static_cast<size_t>(min(i, cd.q_len - 1)) * mk.words + w] : 0u;
+        } else {
+          const int left = mk.clear - k;
+          seen_w[nb] = left >= 32 ? ~0u : left > 0 ? (1u << left) - 1u : 0u;
+        }
+      }
+    }
     uint32_t bad = 0;   // bit r of lane row qd: the values of key 4 qd + r (r >= 4: 12 + 4 qd + r) are not all finite
     bf16x8 vop[DT];
     float vs[8];
@@ -283,20 +297,11 @@ __device__ __forceinline__ void rows_body(const RowsArgs& a) {
       }
       // sa[r]: row c, key k + 4 qd + r; sb[r]: the same + 16.
       float x[8] = {sa[0], sa[1], sa[2], sa[3], sb[0], sb[1], sb[2], sb[3]}, vn[8];
-      uint32_t word = ~0u;
       if constexpr (FP4)
 #pragma unroll
         for (int r = 0; r < 8; ++r) vn[r] = vs[r];
       if (partly) {
-        if (mk.words > 0) {
-          const int w = (k >> 5) - (mk.clear >> 5), i = (16 * nb + c) >> a.group_log2;
-          const uint32_t* words = (const uint32_t*)meta_at<uint32_t>(a.meta, a.words_off) + mk.off;
-          word = w < mk.words ? words[static_cast<size_t>(min(i, cd.q_len - 1)) * mk.words + w] : 0u;
-        } else {
-          const int left = mk.clear - k;
-          if (left < 32) word = left > 0 ? (1u << left) - 1u : 0u;
-        }
-        const uint32_t mine = word >> (4 * qd);
+        const uint32_t mine = seen_w[nb] >> (4 * qd);
 #pragma unroll
         for (int r = 0; r < 8; ++r) {
           const bool in = mine >> (r < 4 ? r : 12 + r) & 1;
@@ -343,7 +348,7 @@ __device__ __forceinline__ void rows_body(const RowsArgs& a) {
               const uint32_t mine = static_cast<uint32_t>((b < 4 ? lo : hi) >> (16 * (b & 3))) << 16;
               const float wt = __int_as_float(__builtin_amdgcn_ds_bpermute((16 * qq + c) << 2, static_cast<int>(mine)));
               const int key = 4 * qq + (b & 3);
-              const bool sees = word >> (key + (b < 4 ? 0 : 16)) & 1;
+              const bool sees = seen_w[nb] >> (key + (b < 4 ? 0 : 16)) & 1;
               const uint16_t* v = reinterpret_cast<const uint16_t*>(base + static_cast<size_t>(__builtin_amdgcn_readlane(pid, b < 4 ? j : min(j + 1, n_pg - 1))) * page_stride) +
                                   kPageTokens * D + key;
 #pragma unroll
@@ -382,41 +387,55 @@ __device__ __forceinline__ void rows_body(const RowsArgs& a) {
     }
   }
 
-  // The eight waves' results are joined 16 rows at a time, each wave those of some rows, in the order of the waves.
+  // The eight waves' results are joined NX blocks at a time, each wave some rows, in the order of the waves. (The joining code is there
+  // once: what a launch runs for the first time has to be fetched, and small launches wait for that.)
   constexpr int LPR = D / 4, RPW = 64 / LPR;   // lanes of a row, rows a wave
+  const int rr = wave * RPW + lane / LPR, d4 = 4 * (lane % LPR);
+#pragma unroll 1
+  for (int nb0 = 0; nb0 < nb_used; nb0 += NX) {
+    if (nb0 > 0) __syncthreads();   // the bytes' last readers
 #pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    if (NB > 1 && nb >= nb_used) break;
-    float (*x)[16][R] = xch[nb % NX];
-    const float l = quarters_sum(l_run[nb]);
+    for (int nb = 0; nb < NB; ++nb) {
+      if (nb / NX * NX != nb0 || nb >= nb_used) continue;
+      float (*x)[R] = xch[nb % NX][wave];
+      const float l = quarters_sum(l_run[nb]);
 #pragma unroll
-    for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4*>(&x[wave][c][16 * t + 4 * qd]) = o[nb][t];
-    if (qd == 0) {
-      x[wave][c][D] = m_run[nb];
-      x[wave][c][D + 1] = l;
+      for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4*>(&x[c][16 * t + 4 * qd]) = o[nb][t];
+      if (qd == 0) *reinterpret_cast<f32x2*>(&x[c][D]) = f32x2{m_run[nb], l};
     }
     __syncthreads();
-    const int rr = wave * RPW + lane / LPR, d4 = 4 * (lane % LPR), r = 16 * nb + rr;
-    if (rr >= 16 || r >= n_rows) continue;
-    float M = x[0][rr][D];
+    if (rr >= 16) continue;
+#pragma unroll 1
+    for (int u = 0; u < NX; ++u) {
+      const int r = 16 * (nb0 + u) + rr;
+      if (r >= n_rows) break;
+      f32x2 ml[kRowWaves];
+      f32x4 y[kRowWaves];
 #pragma unroll
-    for (int w = 1; w < kRowWaves; ++w) M = fmaxf(M, x[w][rr][D]);
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    float den = 0.f;
+      for (int w = 0; w < kRowWaves; ++w) {
+        ml[w] = *reinterpret_cast<const f32x2*>(&xch[u][w][rr][D]);
+        y[w] = *reinterpret_cast<const f32x4*>(&xch[u][w][rr][d4]);
+      }
+      float M = ml[0].x;
 #pragma unroll
-    for (int w = 0; w < kRowWaves; ++w) {
-      const float wt = fast_exp2((x[w][rr][D] - M) * a.scale_log2);
-      const f32x4 y = *reinterpret_cast<const f32x4*>(&x[w][rr][d4]);
-      den = __builtin_fmaf(wt, x[w][rr][D + 1], den);
+      for (int w = 1; w < kRowWaves; ++w) M = fmaxf(M, ml[w].x);
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+      float den = 0.f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[i] = __builtin_fmaf(wt, y[i], acc[i]);
-    }
-    if (mk.rec < 0) {   // the item is the whole conversation
-      st8(a.out + row_offset(r) + d4, make_uint2(pack_bf16x2(acc[0] / den, acc[1] / den), pack_bf16x2(acc[2] / den, acc[3] / den)));
-    } else {
-      float* rec = a.parts + ((static_cast<size_t>(mk.rec + it.k0 / item_keys) * a.n_kv_heads + g) * (16 * NB) + r) * R;
-      __builtin_nontemporal_store(acc, reinterpret_cast<f32x4*>(rec + d4));
-      if (d4 == 0) *reinterpret_cast<f32x2*>(rec + D) = f32x2{M, den};
+      for (int w = 0; w < kRowWaves; ++w) {
+        const float wt = fast_exp2((ml[w].x - M) * a.scale_log2);
+        den = __builtin_fmaf(wt, ml[w].y, den);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] = __builtin_fmaf(wt, y[w][i], acc[i]);
+      }
+      if (mk.rec < 0) {   // the item is the whole conversation
+        const float inv = 1.f / den;
+        st8(a.out + row_offset(r) + d4, make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)));
+      } else {
+        float* rec = a.parts + ((static_cast<size_t>(mk.rec + it.k0 / item_keys) * a.n_kv_heads + g) * (16 * NB) + r) * R;
+        __builtin_nontemporal_store(acc, reinterpret_cast<f32x4*>(rec + d4));
+        if (d4 == 0) *reinterpret_cast<f32x2*>(rec + D) = f32x2{M, den};
+      }
     }
   }
 }
@@ -430,38 +449,41 @@ __global__ __launch_bounds__(64 * kRowWaves) __attribute__((amdgpu_waves_per_eu(
   rows_body<D, NB, true>(a);
 }
 
-// The records of one row of a conversation of several items, joined in a fixed order: one workgroup a row. kv heads fastest, as in the
-// grid that wrote the records.
+// The records of the rows of an entry of several items, joined in a fixed order. A workgroup's 256 threads are SG groups of D / 4
+// lanes (4 dims each); `per_row` of them (a power of two, at most 4 records each where that holds all) share a row. kv heads
+// fastest, as in the grid that wrote the records. (A workgroup a row: 42 us for 64 trees of 64 rows, two or three records a row.)
 template <int D>
-__global__ __launch_bounds__(256) void seen_rows_merge_kernel(LaunchMeta, RowsArgs a, int rows, int rows16) {
+__global__ __launch_bounds__(256) void seen_rows_merge_kernel(LaunchMeta, RowsArgs a, int row_groups, int per_row, int rows16) {
   constexpr int DV = D / 4, SG = 256 / DV, R = partial_floats(D), kAhead = 4;
-  __shared__ MergeLds<D> lds;
-  const int g = blockIdx.x % a.n_kv_heads, r = blockIdx.x / a.n_kv_heads % rows;
-  const int conv = meta_at<int32_t>(a.meta, a.merges_off)[blockIdx.x / a.n_kv_heads / rows];
+  __shared__ float red_m[SG], red_l[SG];
+  __shared__ __attribute__((aligned(16))) float red_o[SG][D];
+  const int tid = threadIdx.x, d4 = 4 * (tid % DV), sg = tid / DV, part = sg % per_row;
+  const int g = blockIdx.x % a.n_kv_heads, rg = blockIdx.x / a.n_kv_heads % row_groups;
+  const int conv = meta_at<int32_t>(a.meta, a.merges_off)[blockIdx.x / a.n_kv_heads / row_groups];
   const ExtendConvDesc cd = a.conv(conv);
-  if (r >= cd.q_len << a.group_log2) return;
+  const int n_rows = cd.q_len << a.group_log2, r0 = rg * (SG / per_row), r = r0 + sg / per_row;
+  if (r0 >= n_rows) return;
   const int item_keys = kRowWaves * a.split, n = (cd.len + item_keys - 1) / item_keys;
   const size_t stride = static_cast<size_t>(a.n_kv_heads) * rows16 * R;
-  const float* base = a.parts + (static_cast<size_t>(a.seen(conv).rec) * a.n_kv_heads + g) * rows16 * R + static_cast<size_t>(r) * R;
-  const int tid = threadIdx.x, dg = tid % DV, sg = tid / DV, lane = tid & 63, wave = tid >> 6;
+  const float* base = a.parts + (static_cast<size_t>(a.seen(conv).rec) * a.n_kv_heads + g) * rows16 * R + static_cast<size_t>(min(r, n_rows - 1)) * R;
   f32x2 ml[kAhead];
   f32x4 v[kAhead];
 #pragma unroll
   for (int k = 0; k < kAhead; ++k) {
-    const int s = sg + k * SG;
+    const int s = part + k * per_row;
     const float* p = base + (s < n ? s : 0) * stride;
     ml[k] = *reinterpret_cast<const f32x2*>(p + D);
-    v[k] = *reinterpret_cast<const f32x4*>(p + 4 * dg);
+    v[k] = *reinterpret_cast<const f32x4*>(p + d4);
   }
-  float M = ml[0].x;
+  float M = ml[0].x;                 // (record 0 where the thread has none)
 #pragma unroll
   for (int k = 1; k < kAhead; ++k) M = fmaxf(M, ml[k].x);
-  for (int s = sg + kAhead * SG; s < n; s += SG) M = fmaxf(M, base[s * stride + D]);
-#pragma unroll
-  for (int off = 32; off >= DV; off >>= 1) M = fmaxf(M, xor_shfl(M, off));
-  if (lane == 0) lds.wave_max[wave] = M;
-  __syncthreads();
-  M = fmaxf(fmaxf(lds.wave_max[0], lds.wave_max[1]), fmaxf(lds.wave_max[2], lds.wave_max[3]));
+  for (int s = part + kAhead * per_row; s < n; s += per_row) M = fmaxf(M, base[s * stride + D]);
+  if (per_row > 1) {
+    if (d4 == 0) red_m[sg] = M;
+    __syncthreads();
+    for (int k = 0; k < per_row; ++k) M = fmaxf(M, red_m[sg - part + k]);
+  }
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   float den = 0.f;
   auto add = [&](f32x2 x, f32x4 y) {
@@ -471,24 +493,25 @@ __global__ __launch_bounds__(256) void seen_rows_merge_kernel(LaunchMeta, RowsAr
   };
 #pragma unroll
   for (int k = 0; k < kAhead; ++k)
-    if (sg + k * SG < n) add(ml[k], v[k]);
+    if (part + k * per_row < n) add(ml[k], v[k]);
 #pragma unroll 4
-  for (int s = sg + kAhead * SG; s < n; s += SG)
-    add(*reinterpret_cast<const f32x2*>(base + s * stride + D), *reinterpret_cast<const f32x4*>(base + s * stride + 4 * dg));
-  *reinterpret_cast<f32x4*>(&lds.red_o[sg][4 * dg]) = acc;
-  if (dg == 0) lds.red_l[sg] = den;
-  __syncthreads();
-  if (tid < D) {
-    float o = 0.f, l = 0.f;
-#pragma unroll
-    for (int k = 0; k < SG; ++k) {
-      o += lds.red_o[k][tid];
-      l += lds.red_l[k];
+  for (int s = part + kAhead * per_row; s < n; s += per_row)
+    add(*reinterpret_cast<const f32x2*>(base + s * stride + D), *reinterpret_cast<const f32x4*>(base + s * stride + d4));
+  if (per_row > 1) {
+    *reinterpret_cast<f32x4*>(&red_o[sg][d4]) = acc;
+    if (d4 == 0) red_l[sg] = den;
+    __syncthreads();
+    if (part != 0) return;
+    for (int k = 1; k < per_row; ++k) {
+      acc += *reinterpret_cast<const f32x4*>(&red_o[sg + k][d4]);
+      den += red_l[sg + k];
     }
-    const int n_q_heads = a.n_kv_heads << a.group_log2;
-    a.out[(static_cast<size_t>(cd.q_row + (r >> a.group_log2)) * n_q_heads + (g << a.group_log2) + (r & ((1 << a.group_log2) - 1))) * D + tid] =
-        static_cast<uint16_t>(pack_bf16x2(o / l, 0.f) & 0xFFFFu);
   }
+  if (r >= n_rows) return;
+  const int n_q_heads = a.n_kv_heads << a.group_log2;
+  uint16_t* row = a.out + (static_cast<size_t>(cd.q_row + (r >> a.group_log2)) * n_q_heads + (g << a.group_log2) + (r & ((1 << a.group_log2) - 1))) * D;
+  const float inv = 1.f / den;
+  st8(row + d4, make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)));
 }
 
 static RowsArgs make_rows_args(const PoolGeom& g, int layer, const SeenLaunch& w, const void* q, void* out, float* parts) {
@@ -530,6 +553,7 @@ hipError_t launch_seen_rows(const PoolGeom& g, int layer, const SeenLaunch& w, c
     };
     if (w.blocks == 1) return launch(std::integral_constant<int, 1>{});
     if (w.blocks == 2) return launch(std::integral_constant<int, 2>{});
+    if (w.blocks == 3) return launch(std::integral_constant<int, 3>{});
     if (w.blocks == 4) return launch(std::integral_constant<int, 4>{});
     return hipErrorInvalidValue;
   };
@@ -542,12 +566,17 @@ hipError_t launch_seen_rows_merge(const PoolGeom& g, const SeenLaunch& w, void* 
   if (w.n_merges == 0) return hipSuccess;
   if (!w.meta.ok() || parts == nullptr) return hipErrorInvalidValue;
   const RowsArgs a = make_rows_args(g, 0, w, nullptr, out, parts);
-  const int64_t n_blocks = static_cast<int64_t>(w.n_merges) * w.merge_rows * g.n_kv_heads;
+  // record groups a row: as many as hold the most records of an entry, four each
+  const int groups = 1024 / g.head_dim;
+  int per_row = 1;
+  while (per_row < groups && 4 * per_row < w.merge_items) per_row *= 2;
+  const int rows = groups / per_row, row_groups = (w.merge_rows + rows - 1) / rows;
+  const int64_t n_blocks = static_cast<int64_t>(w.n_merges) * row_groups * g.n_kv_heads;
   if (!grid_holds(n_blocks, 256)) return hipErrorInvalidConfiguration;
   LaunchMeta m;
   fill_meta(w.meta, &m);
-  if (g.head_dim == 128) seen_rows_merge_kernel<128><<<static_cast<unsigned>(n_blocks), 256, 0, stream>>>(m, a, w.merge_rows, 16 * w.blocks);
-  else if (g.head_dim == 64) seen_rows_merge_kernel<64><<<static_cast<unsigned>(n_blocks), 256, 0, stream>>>(m, a, w.merge_rows, 16 * w.blocks);
+  if (g.head_dim == 128) seen_rows_merge_kernel<128><<<static_cast<unsigned>(n_blocks), 256, 0, stream>>>(m, a, row_groups, per_row, 16 * w.blocks);
+  else if (g.head_dim == 64) seen_rows_merge_kernel<64><<<static_cast<unsigned>(n_blocks), 256, 0, stream>>>(m, a, row_groups, per_row, 16 * w.blocks);
   else return hipErrorInvalidValue;
   return hipGetLastError();
 }
