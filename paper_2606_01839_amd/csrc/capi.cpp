@@ -948,7 +948,7 @@ cs_status run_seen_rows(cs_pool* p, const std::vector<SeenEntry>& entries, int32
     cs::SeenLaunch w;
     std::vector<int32_t> slots;
     std::vector<int64_t> lens;
-    for (;; e = e0 + (e - e0) / 2) {
+    for (int32_t split = 0;;) {
       slots.clear();
       lens.clear();
       rows = 0;
@@ -959,11 +959,14 @@ cs_status run_seen_rows(cs_pool* p, const std::vector<SeenEntry>& entries, int32
       }
       w.blocks = (rows + 15) / 16;
       if (e == e0) break;
-      plan = cs::decode_plan_of(slots, lens, cs::rows_split(lens, g.n_kv_heads, cs::kCus));
+      // (long items first need fewer records, then fewer entries do)
+      split = split == 0 ? cs::rows_split(lens, g.n_kv_heads, cs::kCus) : 1024;
+      plan = cs::decode_plan_of(slots, lens, split);
       size_t records = 0;
       for (const auto& c : plan.convs) records += c.n_splits > 1 ? c.n_splits : 0;
       if (records * g.n_kv_heads * 16 * w.blocks * cs::partial_floats(g.head_dim) <= room &&
           plan.n_items * sizeof(cs::SeenItem) <= kQuarter / 2) break;
+      if (split == 1024) e = e0 + (e - e0) / 2;
     }
     if (e == e0) {
       tiles->push_back(entries[e0++]);
@@ -1370,7 +1373,8 @@ cs_status cs_kv_keep(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t*
   // What moves: from the first token that does not stay where it is. A last page that ends before its slots do is
   // rewritten too, with zeros behind the end.
   std::vector<cs::KeepConv> work;
-  std::vector<int32_t> src;
+  std::vector<int32_t> pages;
+  std::vector<int64_t> src;
   std::vector<int64_t> new_len(static_cast<size_t>(n));
   std::vector<std::vector<int32_t>> dropped(static_cast<size_t>(n));
   at = keep;
@@ -1384,9 +1388,16 @@ cs_status cs_kv_keep(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t*
       dropped[i].assign(cv[i]->pages.begin() + lp1, cv[i]->pages.end());
       const int64_t lp0 = first / cs::kPage;
       if (lp1 > lp0) {
-        work.push_back({cs::ConvTable::slot_of(convs[i]), static_cast<int32_t>(lp0), static_cast<int32_t>(lp1 - lp0),
-                        static_cast<int32_t>(first), static_cast<int32_t>(len), static_cast<int32_t>(src.size())});
-        for (int32_t x = j; x < n_keep[i]; ++x) src.push_back(static_cast<int32_t>(base + at[x]));
+        const std::vector<int32_t>& own = cv[i]->pages;
+        const int64_t from = first & ~int64_t(7);   // half a page's slots are written at once
+        work.push_back({static_cast<int32_t>(pages.size()), static_cast<int32_t>(lp1 - lp0), static_cast<int32_t>(first - lp0 * cs::kPage),
+                        static_cast<int32_t>(len - lp0 * cs::kPage), static_cast<int32_t>(from - lp0 * cs::kPage),
+                        static_cast<int32_t>(src.size())});
+        pages.insert(pages.end(), own.begin() + lp0, own.begin() + lp1);
+        for (int64_t s = from; s < len; ++s) {
+          const int64_t f = s < first ? s : base + at[s - base];
+          src.push_back(static_cast<int64_t>(own[static_cast<size_t>(f / cs::kPage)]) * cs::kPage + f % cs::kPage);
+        }
       }
     }
     if (n_keep[i] > 0) at += n_keep[i];
@@ -1394,6 +1405,7 @@ cs_status cs_kv_keep(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t*
   if (!work.empty()) {
     Blob b;
     b.push(work.data(), work.size());
+    const size_t pages_off = b.push(pages.data(), pages.size());
     const size_t src_off = b.push(src.data(), src.size());
     if (b.bytes.size() > kQuarter) return fail(CS_ENOMEM, "batch descriptor exceeds the metadata ring");
     if ((st = ensure_device(p)) != CS_OK) return st;
@@ -1404,7 +1416,7 @@ cs_status cs_kv_keep(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t*
     cs::Meta m;
     if ((st = place_meta(p, b, &m)) != CS_OK) return st;
     st = timed_launch(p, CS_PROF_APPEND, "keep launch",
-                      [&] { return cs::launch_keep(p->geom(), m, src_off, static_cast<int>(work.size()), p->stream); });
+                      [&] { return cs::launch_keep(p->geom(), m, pages_off, src_off, static_cast<int>(work.size()), p->stream); });
     if (st != CS_OK) return st;
   }
   for (int32_t i = 0; i < n; ++i) {   // (allocates nothing)

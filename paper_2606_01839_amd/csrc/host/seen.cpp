@@ -5,8 +5,12 @@
 namespace cs {
 
 int32_t rows_split(const std::vector<int64_t>& lens, int32_t n_kv_heads, int32_t n_cus) {
-  int64_t keys = 0;
-  for (const int64_t n : lens) keys += n;
+  int64_t keys = 0, longest = 0;
+  for (const int64_t n : lens) {
+    keys += n;
+    longest = std::max(longest, n);
+  }
+  if (longest <= 64 * kDecodeSubSplits) return 64;
   const int64_t share = keys * n_kv_heads / n_cus;   // of a CU
   for (const int64_t most : {2 * n_cus, 3 * n_cus, 4 * n_cus}) {   // twice the workgroups
     for (int32_t split = 32; split <= 1024; split += 32) {

@@ -91,15 +91,14 @@ struct RopeConv {
 hipError_t launch_rope_q(const PoolGeom& g, const Meta& meta, int n_convs, int64_t rows, int n_layers, const RopeArgs& rope,
                          const void* q, void* out, hipStream_t stream);
 
-// Keep of drafted tokens: meta = KeepConv[n_convs], then at src_off the source slots of the moved tokens.
+// Keep of drafted tokens: meta = KeepConv[n_convs], at pages_off int32 physical pages, at src_off int64 sources (16 x physical page
+// + token slot).
 struct KeepConv {
-  int32_t slot;     // row of the page table
-  int32_t lp0, n_lp;   // logical pages that are rewritten
-  int32_t first;    // first token slot of the conversation that changes
-  int32_t len;      // its new length: slots [first, len) receive tokens, those behind them zeros
-  int32_t src;      // source slot of slot `first` + i: entry src + i
+  int32_t page0, n;    // the pages that are rewritten: entries page0 .. page0 + n - 1, in order
+  int32_t first, len;  // token slots, counted from the first of those pages': [first, len) receive tokens, those behind them zeros
+  int32_t from, src;   // source of slot from + i (from: first rounded down to 8; a slot before `first` is its own): entry src + i
 };
-hipError_t launch_keep(const PoolGeom& g, const Meta& meta, size_t src_off, int n_convs, hipStream_t stream);
+hipError_t launch_keep(const PoolGeom& g, const Meta& meta, size_t pages_off, size_t src_off, int n_convs, hipStream_t stream);
 
 // Workgroups that the queries of an append of n_chunks add to its launch.
 int64_t append_rope_groups(const PoolGeom& g, size_t n_chunks);

@@ -68,6 +68,8 @@ __device__ __forceinline__ void rows_body(const RowsArgs& a) {
   constexpr int QW = FP4 ? 5 : KS;          // 16-byte words of a lane's query operand, a block
   constexpr int NX = NB > 1 ? 2 : 1;        // blocks the waves exchange at a time
   __shared__ __attribute__((aligned(16))) float xch[NX][kRowWaves][16][R];
+  constexpr bool WLDS = NB > 3 && !FP4;     // words in LDS: the registers are full
+  __shared__ uint32_t w_lds[WLDS ? kRowWaves : 1][WLDS ? NB : 1][16];
   __shared__ uint4 q_lds[QLDS ? NB : 1][QLDS ? QW : 1][64];
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -210,24 +212,27 @@ __device__ __forceinline__ void rows_body(const RowsArgs& a) {
   auto step = [&](const Page& pa, const Page& pb, const int j) {
     const int k = k_begin + kPageTokens * j;
     const bool partly = k + 2 * kPageTokens > mk.clear;
-    uint32_t seen_w[NB];   // of the lane's rows, for the 32 keys
+    uint32_t seen_w[WLDS ? 1 : NB];   // of the lane's rows, for the 32 keys
     if (partly) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
+        uint32_t word;
         if (mk.words > 0) {
           const int w = (k >> 5) - (mk.clear >> 5), i = (16 * nb + c) >> a.group_log2;
           const uint32_t* words = (const uint32_t*)meta_at<uint32_t>(a.meta, a.words_off) + mk.off;
-          seen_w[nb] = w < mk.words ? words[static_cast<size_t>(min(i, cd.q_len - 1)) * mk.words + w] : 0u;
+          word = w < mk.words ? words[static_cast<size_t>(min(i, cd.q_len - 1)) * mk.words + w] : 0u;
         } else {
           const int left = mk.clear - k;
-          seen_w[nb] = left >= 32 ? ~0u : left > 0 ? (1u << left) - 1u : 0u;
+          word = left >= 32 ? ~0u : left > 0 ? (1u << left) - 1u : 0u;
         }
+        if constexpr (WLDS) w_lds[wave][nb][c] = word;
+        else seen_w[nb] = word;
       }
     }
+    auto word_of = [&](int nb) { return WLDS ? w_lds[wave][nb][c] : seen_w[WLDS ? 0 : nb]; };
     uint32_t bad = 0;   // bit r of lane row qd: the values of key 4 qd + r (r >= 4: 12 + 4 qd + r) are not all finite
     bf16x8 vop[DT];
-    float vs[8];
-    if constexpr (FP4) {
+    auto convert = [&]() {
       const uint32_t wa[4] = {pa.v[0].x, pa.v[0].y, pa.v[1].x, pa.v[1].y}, wb[4] = {pb.v[0].x, pb.v[0].y, pb.v[1].x, pb.v[1].y};
 #pragma unroll
       for (int w = 0; w < NW; ++w) {
@@ -236,8 +241,9 @@ __device__ __forceinline__ void rows_body(const RowsArgs& a) {
         vop[2 * w + 1] = as_bf16x8(make_uint2(fp4_pair<2>(wa[w], 1.f), fp4_pair<3>(wa[w], 1.f)),
                                    make_uint2(fp4_pair<2>(wb[w], 1.f), fp4_pair<3>(wb[w], 1.f)));
       }
-#pragma unroll
-      for (int r = 0; r < 8; ++r) vs[r] = fp4_scale_of(r < 4 ? pa.vs : pb.vs, r % 4);
+    };
+    if constexpr (FP4) {
+      if constexpr (NB > 1) convert();   // once for all blocks (one block: where it is used, two workgroups a CU)
     } else {
 #pragma unroll
       for (int t = 0; t < DT; ++t) vop[t] = pages_v(pa.v[t], pb.v[t]);
@@ -299,9 +305,9 @@ __device__ __forceinline__ void rows_body(const RowsArgs& a) {
       float x[8] = {sa[0], sa[1], sa[2], sa[3], sb[0], sb[1], sb[2], sb[3]}, vn[8];
       if constexpr (FP4)
 #pragma unroll
-        for (int r = 0; r < 8; ++r) vn[r] = vs[r];
+        for (int r = 0; r < 8; ++r) vn[r] = fp4_scale_of(r < 4 ? pa.vs : pb.vs, r % 4);
       if (partly) {
-        const uint32_t mine = seen_w[nb] >> (4 * qd);
+        const uint32_t mine = word_of(nb) >> (4 * qd);
 #pragma unroll
         for (int r = 0; r < 8; ++r) {
           const bool in = mine >> (r < 4 ? r : 12 + r) & 1;
@@ -348,7 +354,7 @@ __device__ __forceinline__ void rows_body(const RowsArgs& a) {
               const uint32_t mine = static_cast<uint32_t>((b < 4 ? lo : hi) >> (16 * (b & 3))) << 16;
               const float wt = __int_as_float(__builtin_amdgcn_ds_bpermute((16 * qq + c) << 2, static_cast<int>(mine)));
               const int key = 4 * qq + (b & 3);
-              const bool sees = seen_w[nb] >> (key + (b < 4 ? 0 : 16)) & 1;
+              const bool sees = word_of(nb) >> (key + (b < 4 ? 0 : 16)) & 1;
               const uint16_t* v = reinterpret_cast<const uint16_t*>(base + static_cast<size_t>(__builtin_amdgcn_readlane(pid, b < 4 ? j : min(j + 1, n_pg - 1))) * page_stride) +
                                   kPageTokens * D + key;
 #pragma unroll
@@ -366,6 +372,7 @@ __device__ __forceinline__ void rows_body(const RowsArgs& a) {
                         pack_bf16x2(p[4] * vn[4], p[5] * vn[5]), pack_bf16x2(p[6] * vn[6], p[7] * vn[7]));
       }
       const bf16x8 pop = __builtin_bit_cast(bf16x8, pw);
+      if constexpr (FP4 && NB == 1) convert();
 #pragma unroll
       for (int t = 0; t < DT; ++t) o[nb][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vop[t], pop, o[nb][t], 0, 0, 0);
     }
