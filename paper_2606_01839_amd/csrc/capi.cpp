@@ -1049,6 +1049,16 @@ cs_status run_seen(cs_pool* p, const std::vector<SeenEntry>& entries, bool all, 
                         [&] { return cs::launch_seen_empty(p->geom(), m, static_cast<int>(n), out, p->stream); });
     if (st != CS_OK) return st;
   }
+  // Both kinds in one batch take four launches one after the other: the few-row entries join the tiles where those hold more keys
+  // (16 trees of 17 to 100 tokens, 16 query and 8 kv heads, over 4-bit pages of 1k-9k: 72.7 us against 76).
+  int64_t row_keys = 0, tile_keys = 0;
+  for (const SeenEntry& x : rows) row_keys += x.len;
+  for (const SeenEntry& x : tiles) tile_keys += x.len;
+  if (row_keys <= tile_keys) {
+    tiles.insert(tiles.end(), rows.begin(), rows.end());
+    std::sort(tiles.begin(), tiles.end(), [](const SeenEntry& a, const SeenEntry& b) { return a.q_row < b.q_row; });
+    rows.clear();
+  }
   const cs_status st = run_seen_rows(p, rows, layer, q, out, &tiles);
   return st == CS_OK ? run_seen_tiles(p, tiles, all, layer, q, out) : st;
 }

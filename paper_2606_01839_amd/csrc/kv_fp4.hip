@@ -49,6 +49,7 @@ struct AppendArgs {
   int n_layers, n_kv_heads, n_q_heads;
   int kv_blocks;   // grid rows of the K and V; the queries' follow
   int q_groups;    // grid rows a layer of the queries
+  int q_heads;     // query heads a workgroup rotates
   uint4* carry_dst;
   int carry_off, carry_n16;
   const uint16_t* k;
@@ -127,8 +128,8 @@ __global__ __launch_bounds__(256) void kv_append_as_kernel(LaunchMeta, RopeArgs 
   if (ROPE && static_cast<int>(blockIdx.y) >= a.kv_blocks) {
     rope_table<D>(tab, CH * kPageTokens, rope, waves, row_pos);
     const int y = blockIdx.y - a.kv_blocks;
-    const int layer = y / a.q_groups, h0 = y % a.q_groups * kQHeads;
-    for (int h = h0 + wave; h < min(h0 + kQHeads, a.n_q_heads); h += waves) {
+    const int layer = y / a.q_groups, h0 = y % a.q_groups * a.q_heads;
+    for (int h = h0 + wave; h < min(h0 + a.q_heads, a.n_q_heads); h += waves) {
       uint4 x[CH][kPasses];
 #pragma unroll
       for (int i = 0; i < CH; ++i)
@@ -569,7 +570,10 @@ hipError_t launch_append_as(const PoolGeom& g, const Meta& meta, int n_chunks, c
   a.n_kv_heads = g.n_kv_heads;
   a.n_q_heads = g.n_q_heads;
   a.kv_blocks = g.n_layers * (g.n_kv_heads / waves);
-  a.q_groups = (g.n_q_heads + kQHeads - 1) / kQHeads;
+  // One head a wave where that leaves CUs without work: a wave's heads come one after the other.
+  const int64_t chunk_groups = (n_chunks + kChunks - 1) / kChunks;
+  a.q_heads = chunk_groups * g.n_layers * ((g.n_q_heads + waves - 1) / waves) <= kCus ? waves : kQHeads;
+  a.q_groups = (g.n_q_heads + a.q_heads - 1) / a.q_heads;
   a.carry_dst = static_cast<uint4*>(carry.dst);
   a.carry_off = static_cast<int>(carry.off);
   a.carry_n16 = static_cast<int>(carry.bytes / 16);

@@ -102,6 +102,47 @@ __device__ __forceinline__ void rows_body(const RowsArgs& a) {
       for (int i = 0; i < KS; ++i) x[i] = ld16(FP4 ? p + D / 4 * qd + 8 * i : p + 32 * i + 8 * qd);
     }
   };
+  using B = Fp4Block<D>;
+  constexpr int NW = B::kWords;
+  const size_t block_bytes = FP4 ? B::kBytes : 4 * kPageTokens * D;
+  const size_t page_stride = static_cast<size_t>(a.n_kv_heads) * block_bytes;
+  const uint8_t* base = reinterpret_cast<const uint8_t*>(a.pool) + static_cast<size_t>(a.layer) * a.n_pages * page_stride +
+                        static_cast<size_t>(g) * block_bytes;
+  const uint32_t koff = (c * 32 + 8 * qd) * 2, voff = (kPageTokens * D + c * kPageTokens + 4 * qd) * 2;
+  const uint32_t f_k = B::k_lane(lane), f_v = B::kV + lane * 4 * NW, f_ks = B::k_scale_lane(lane), f_vs = B::kVScale + 4 * qd;
+  struct Page {
+    u32x4_t k[FP4 ? 1 : KS];
+    u32x2_t v[FP4 ? 2 : DT];
+    uint32_t ks, vs;
+  };
+  auto load = [&](int j) {
+    Page p;
+    const uint8_t* blk = base + static_cast<size_t>(__builtin_amdgcn_readlane(pid, j)) * page_stride;
+    p.ks = p.vs = 0;
+    if constexpr (FP4) {
+      // (as 32-bit offsets to a scalar base; hoisted out of the loop they would be widened to register pairs)
+      uint32_t ok = f_k, ov = f_v, oks = f_ks, ovs = f_vs;
+      asm volatile("" : "+v"(ok), "+v"(ov), "+v"(oks), "+v"(ovs));
+      if constexpr (D == 128) {
+        const u32x4_t v = nt16(blk + ov);
+        p.k[0] = nt16(blk + ok);
+        p.v[0] = v.lo, p.v[1] = v.hi;
+      } else {
+        const u32x2_t k = nt8(blk + ok);
+        p.k[0] = u32x4_t{k.x, k.y, 0, 0};
+        p.v[0] = nt8(blk + ov), p.v[1] = u32x2_t{0, 0};
+      }
+      p.ks = blk[oks];
+      p.vs = *reinterpret_cast<const uint32_t*>(blk + ovs);
+    } else {
+#pragma unroll
+      for (int i = 0; i < KS; ++i) p.k[i] = nt16(blk + koff + 1024 * i);
+#pragma unroll
+      for (int t = 0; t < DT; ++t) p.v[t] = nt8(blk + voff + 16 * kPageTokens * 2 * t);
+    }
+    return p;
+  };
+
   struct Query {
     bf16x8 b[KS];
     Bf6Query x;
@@ -166,47 +207,6 @@ __device__ __forceinline__ void rows_body(const RowsArgs& a) {
     for (int t = 0; t < DT; ++t) o[nb][t] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   const bf16x2 ones = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
-
-  using B = Fp4Block<D>;
-  constexpr int NW = B::kWords;
-  const size_t block_bytes = FP4 ? B::kBytes : 4 * kPageTokens * D;
-  const size_t page_stride = static_cast<size_t>(a.n_kv_heads) * block_bytes;
-  const uint8_t* base = reinterpret_cast<const uint8_t*>(a.pool) + static_cast<size_t>(a.layer) * a.n_pages * page_stride +
-                        static_cast<size_t>(g) * block_bytes;
-  const uint32_t koff = (c * 32 + 8 * qd) * 2, voff = (kPageTokens * D + c * kPageTokens + 4 * qd) * 2;
-  const uint32_t f_k = B::k_lane(lane), f_v = B::kV + lane * 4 * NW, f_ks = B::k_scale_lane(lane), f_vs = B::kVScale + 4 * qd;
-  struct Page {
-    u32x4_t k[FP4 ? 1 : KS];
-    u32x2_t v[FP4 ? 2 : DT];
-    uint32_t ks, vs;
-  };
-  auto load = [&](int j) {
-    Page p;
-    const uint8_t* blk = base + static_cast<size_t>(__builtin_amdgcn_readlane(pid, j)) * page_stride;
-    p.ks = p.vs = 0;
-    if constexpr (FP4) {
-      // (as 32-bit offsets to a scalar base; hoisted out of the loop they would be widened to register pairs)
-      uint32_t ok = f_k, ov = f_v, oks = f_ks, ovs = f_vs;
-      asm volatile("" : "+v"(ok), "+v"(ov), "+v"(oks), "+v"(ovs));
-      if constexpr (D == 128) {
-        const u32x4_t v = nt16(blk + ov);
-        p.k[0] = nt16(blk + ok);
-        p.v[0] = v.lo, p.v[1] = v.hi;
-      } else {
-        const u32x2_t k = nt8(blk + ok);
-        p.k[0] = u32x4_t{k.x, k.y, 0, 0};
-        p.v[0] = nt8(blk + ov), p.v[1] = u32x2_t{0, 0};
-      }
-      p.ks = blk[oks];
-      p.vs = *reinterpret_cast<const uint32_t*>(blk + ovs);
-    } else {
-#pragma unroll
-      for (int i = 0; i < KS; ++i) p.k[i] = nt16(blk + koff + 1024 * i);
-#pragma unroll
-      for (int t = 0; t < DT; ++t) p.v[t] = nt8(blk + voff + 16 * kPageTokens * 2 * t);
-    }
-    return p;
-  };
 
   // Keys k .. k + 31: pages j, j + 1 (a last single page stands in for its second, whose keys are not seen).
   auto step = [&](const Page& pa, const Page& pb, const int j) {
@@ -378,7 +378,7 @@ __device__ __forceinline__ void rows_body(const RowsArgs& a) {
     }
   };
   if constexpr (FP4) {
-    if (n_pg > 0) {
+    if (n_pg > 0) {   // the next pages fly during a step
       Page a0 = load(0), b0 = load(min(1, n_pg - 1));
       for (int j = 0; j < n_pg; j += 2) {
         const Page pa = a0, pb = b0;
