@@ -1056,11 +1056,12 @@ cs_status run_seen(cs_pool* p, const std::vector<SeenEntry>& entries, bool all, 
   for (const SeenEntry& x : tiles) tile_keys += x.len;
   if (row_keys <= tile_keys) {
     tiles.insert(tiles.end(), rows.begin(), rows.end());
-    std::sort(tiles.begin(), tiles.end(), [](const SeenEntry& a, const SeenEntry& b) { return a.q_row < b.q_row; });
     rows.clear();
   }
   const cs_status st = run_seen_rows(p, rows, layer, q, out, &tiles);
-  return st == CS_OK ? run_seen_tiles(p, tiles, all, layer, q, out) : st;
+  if (st != CS_OK) return st;
+  std::sort(tiles.begin(), tiles.end(), [](const SeenEntry& a, const SeenEntry& b) { return a.q_row < b.q_row; });
+  return run_seen_tiles(p, tiles, all, layer, q, out);
 }
 
 cs_status attend_seen(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t* q_lens, const int32_t* parents, bool tree,
@@ -1412,6 +1413,11 @@ cs_status cs_kv_keep(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t*
     }
     if (n_keep[i] > 0) at += n_keep[i];
   }
+  if (p->dev_ready) {   // (a conversation with tokens has been on the device)
+    hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+    CS_HIP(hipStreamIsCapturing(as_stream(stream), &cap), "hipStreamIsCapturing");
+    if (cap != hipStreamCaptureStatusNone) return fail(CS_ESTATE, "kv_keep cannot be captured: a replay would move the tokens again");
+  }
   if (!work.empty()) {
     Blob b;
     b.push(work.data(), work.size());
@@ -1419,9 +1425,6 @@ cs_status cs_kv_keep(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t*
     const size_t src_off = b.push(src.data(), src.size());
     if (b.bytes.size() > kQuarter) return fail(CS_ENOMEM, "batch descriptor exceeds the metadata ring");
     if ((st = ensure_device(p)) != CS_OK) return st;
-    hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
-    CS_HIP(hipStreamIsCapturing(as_stream(stream), &cap), "hipStreamIsCapturing");
-    if (cap != hipStreamCaptureStatusNone) return fail(CS_ESTATE, "kv_keep cannot be captured: a replay would move the tokens again");
     if ((st = use_stream(p, as_stream(stream))) != CS_OK) return st;
     cs::Meta m;
     if ((st = place_meta(p, b, &m)) != CS_OK) return st;

@@ -48,6 +48,7 @@ extern "C" int words(const int* p, int n, long prefix, unsigned* out) {
   for (size_t i = 3; i < v.size(); ++i) out[i - 3] = v[i];
   return w;
 }
+extern "C" int split(const long* p, int n, int heads) { return cs::rows_split(std::vector<int64_t>(p, p + n), heads, cs::kCus); }
 extern "C" int ok(const int* p, int n) { return cs::tree_ok(p, n); }
 extern "C" void depths(const int* p, int n, int* out) { cs::tree_depths(p, n, out); }
 ''')
@@ -151,3 +152,33 @@ def test_calls_refused():
         assert rc == CS_EINVAL
     assert p.conv_len(a) == 0 and p.occupancy() == (0, 32)
     p.close()
+
+
+CALLS = {
+    "attn_tree": "_, h = pool(64); print(lib.cs_attn_tree(h, N, 4096, 4096, 4096, 0, 4096, 4096, None), None)",
+    "attn_cross": "_, h = pool(64); print(lib.cs_attn_cross(h, N, 4096, 4096, 0, 4096, 4096, None), None)",
+    "kv_keep": "_, h = pool(64); print(lib.cs_kv_keep(h, N, 4096, 4096, 4096, 4096, None), None)",
+    "kv_append_tree": """
+_, h = pool(64); r = RopeDesc(); lib.cs_rope_init(ctypes.byref(r), 64, 0, 1e4, 0, 1., 0., 0., 0.)
+print(lib.cs_kv_append_tree(h, ctypes.byref(r), N, 4096, 4096, 4096, 4096, 4096, None, None, None), None)""",
+}
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_out_of_host_memory(name):
+    """No exception leaves the C ABI, as in test_no_throw_cpu."""
+    import sys
+
+    from tests.test_no_throw_cpu import PRELUDE
+    r = subprocess.run([sys.executable, "-c", PRELUDE + CALLS[name]], capture_output=True, text=True, timeout=120, cwd=ROOT)
+    assert r.returncode == 0, r.stderr[-2000:]
+    assert r.stdout.split() == ["-2", "None"], r.stdout
+
+
+@pytest.mark.parametrize("lens,heads,want", [([300, 512], 8, 64), ([24571], 8, 96), ([1000] * 300, 8, 1024), ([9000, 300], 2, 32), ([1], 1, 64)])
+def test_items_of_few_rows(host, lens, heads, want):
+    """Keys per wave: one round of the 256 CUs where there is one."""
+    a = (ctypes.c_int64 * len(lens))(*lens)
+    split = host.split(a, len(lens), heads)
+    assert split == want, split
+    assert split % 32 == 0 and 32 <= split <= 1024
