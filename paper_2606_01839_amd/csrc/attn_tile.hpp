@@ -118,7 +118,8 @@ __device__ __forceinline__ void lds_wait_barrier() { asm volatile("s_waitcnt lgk
 //
 // SEEN: the rows see what their words say (host/seen.hpp) in place of the keys up to their own: a tree's tokens, or every key.
 // Only tiles that reach past the keys that all rows see test bits, one word a row and 32 keys. There a value that is
-// not finite must not meet a weight of 0: such keys' V operands are cleared and their products added by themselves.
+// not finite must not meet a weight of 0: it is cleared in the operands and added after the last tile to the rows that see it (any
+// weight of an infinity is an infinity).
 template <int D, int G, bool PRE, bool CHAIN, bool FP4 = false, bool SEEN = false>
 __device__ __forceinline__ void attn_fwd_block(const std::conditional_t<SEEN, SeenTileArgs, ExtendArgs>& a, const int block, const int dl) {
   constexpr int NW = 8;                   // waves: G query heads x (8 / G) blocks of 32 queries
@@ -329,6 +330,7 @@ __device__ __forceinline__ void attn_fwd_block(const std::conditional_t<SEEN, Se
   // sees no key of a piece's first tiles keeps weights of 0 (no inf - inf).
   float m_s = -FLT_MAX, l_run = 0.f;
   bool far = false;   // a row's maximum is past kFarScore
+  bool sick = false;  // SEEN: values that are not finite were cleared
   const bf16x2 ones = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
 
   // Start of a step: the tile three (4-bit pages: two) ahead goes on its way into the ring.
@@ -539,7 +541,6 @@ __device__ __forceinline__ void attn_fwd_block(const std::conditional_t<SEEN, Se
     l_run += ps;
     if constexpr (SEEN) {
       if (partly && mk.words > 0) {
-        // Bits 8 (2 kt2 + j2) + i: key 32 kt2 + 16 j2 + 8 half + i of the tile has a value that is not finite (of any lane's dims).
         uint32_t any = 0;
 #pragma unroll
         for (int kt2 = 0; kt2 < 2; ++kt2)
@@ -547,70 +548,22 @@ __device__ __forceinline__ void attn_fwd_block(const std::conditional_t<SEEN, Se
           for (int j2 = 0; j2 < 2; ++j2)
 #pragma unroll
             for (int t = 0; t < DT; ++t) {
-              const uint4 x = __builtin_bit_cast(uint4, vop[kt2][j2][t]);
-              any |= not_finite(x.x) | not_finite(x.y) | not_finite(x.z) | not_finite(x.w);
+              const u32x4_t x = __builtin_bit_cast(u32x4_t, vop[kt2][j2][t]);
+              any |= not_finite(x[0]) | not_finite(x[1]) | not_finite(x[2]) | not_finite(x[3]);
             }
         if (__builtin_expect(__builtin_amdgcn_ballot_w64(any != 0) != 0, false)) {
-          uint32_t bad = 0;
+          sick = true;
 #pragma unroll
           for (int kt2 = 0; kt2 < 2; ++kt2)
 #pragma unroll
             for (int j2 = 0; j2 < 2; ++j2)
 #pragma unroll
               for (int t = 0; t < DT; ++t) {
-                const uint4 x = __builtin_bit_cast(uint4, vop[kt2][j2][t]);
-                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                u32x4_t x = __builtin_bit_cast(u32x4_t, vop[kt2][j2][t]);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  const uint32_t f = not_finite(w[i]);
-                  bad |= ((f >> 15 & 1) | (f >> 31) << 1) << (8 * (2 * kt2 + j2) + 2 * i);
-                }
+                for (int i = 0; i < 4; ++i) x[i] = finite_or_zero(x[i]);
+                vop[kt2][j2][t] = __builtin_bit_cast(bf16x8, x);
               }
-          for (int off = 1; off < 32; off <<= 1) bad |= __float_as_uint(xor_shfl(__uint_as_float(bad), off));
-#pragma unroll
-          for (int kt2 = 0; kt2 < 2; ++kt2)
-#pragma unroll
-            for (int j2 = 0; j2 < 2; ++j2)
-#pragma unroll
-              for (int t = 0; t < DT; ++t) {
-                uint4 x = __builtin_bit_cast(uint4, vop[kt2][j2][t]);
-                const uint32_t m = ~bad >> (8 * (2 * kt2 + j2));
-                x.x = mask_bf16x2(x.x, m & 1, m >> 1 & 1), x.y = mask_bf16x2(x.y, m >> 2 & 1, m >> 3 & 1);
-                x.z = mask_bf16x2(x.z, m >> 4 & 1, m >> 5 & 1), x.w = mask_bf16x2(x.w, m >> 6 & 1, m >> 7 & 1);
-                vop[kt2][j2][t] = as_bf16x8(x);
-              }
-          for (int hh = 0; hh < 2; ++hh) {
-            uint32_t left = __builtin_amdgcn_readlane(bad, 32 * hh);
-            while (left != 0) {
-              const int b = __builtin_ctz(left);
-              left &= left - 1;
-              uint32_t pair = 0;   // the lane's weights of keys b, b ^ 1 of its half
-#pragma unroll
-              for (int kt2 = 0; kt2 < 2; ++kt2)
-#pragma unroll
-                for (int j2 = 0; j2 < 2; ++j2) {
-                  const uint4 x = __builtin_bit_cast(uint4, pop[kt2][j2]);
-                  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                  for (int i = 0; i < 4; ++i)
-                    if (b / 2 == 4 * (2 * kt2 + j2) + i) pair = w[i];
-                }
-              const float mine = b & 1 ? bf16_hi(pair) : bf16_lo(pair);
-              const float wt = __int_as_float(__builtin_amdgcn_ds_bpermute((32 * hh + col) << 2, __float_as_int(mine)));
-              const int kt = b >> 4, in = 16 * (b >> 3 & 1) + 8 * hh + (b & 7);
-              const bool sees = (kt ? seen_w[1] : seen_w[0]) >> in & 1;
-              const uint8_t* vb = smem + VBASE + buf * HALF_TILE + DT * (b >> 3) * 1024 + 2 * (b & 7);
-#pragma unroll
-              for (int t = 0; t < DT; ++t)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                  const int dc = 8 * (e >> 2) + 4 * half + (e & 3);
-                  const uint32_t x = *reinterpret_cast<const uint16_t*>(vb + t * 1024 + dc * 32 + ((hh ^ (dc >> 2 & 1) ^ (dc >> 3 & 1)) * 16));
-                  if (sees) o[t][e] = __builtin_fmaf(wt, __uint_as_float(x << 16), o[t][e]);
-                }
-            }
-          }
-          lds_wait();   // the buffer's reads return before the barrier behind which it is copied over
         }
       }
     }
@@ -675,6 +628,25 @@ __device__ __forceinline__ void attn_fwd_block(const std::conditional_t<SEEN, Se
   // no copy may land after the workgroup ends, nor in what follows
   dma_wait_barrier<0>();
 
+  if constexpr (SEEN) {
+    if (__builtin_expect(sick, false)) {
+      const uint32_t* row = a.words() + mk.off + static_cast<size_t>(valid ? qrow0 + col : cd.q_len - 1) * mk.words;
+      for (int key = kBN * max(mk.clear / kBN, kt0); key < min(cd.len, kBN * n_kt); ++key) {   // of the masked tiles
+        const bool sees = key < mk.clear || (row[(key >> 5) - (mk.clear >> 5)] >> (key & 31) & 1);
+        const int page = ptc[key / kPageTokens], in = key % kPageTokens;
+        const bool nan4 = FP4 && f_base[static_cast<size_t>(page) * f_stride + B4::kVScale + in] == 255;
+        const uint16_t* v = a.pool + layer_base + static_cast<size_t>(page) * page_stride + kPageTokens * D + in;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int dim = 32 * t + 8 * (e >> 2) + 4 * half + (e & 3);
+            const uint32_t x = FP4 ? (nan4 ? 0x7FC0u : 0u) : v[dim * kPageTokens];
+            if (sees && (x & 0x7F80u) == 0x7F80u) o[t][e] += __uint_as_float(x << 16);
+          }
+      }
+    }
+  }
   if (tile.part >= 0) {
     write_record();
     return;

@@ -85,6 +85,12 @@ __device__ __forceinline__ uint32_t mask_bf16x2(uint32_t w, bool keep_lo, bool k
 // Bits 15 and 31: the bf16 value in the low, high half of w is an infinity or NaN.
 __device__ __forceinline__ uint32_t not_finite(uint32_t w) { return ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }
 
+// w with such halves cleared.
+__device__ __forceinline__ uint32_t finite_or_zero(uint32_t w) {
+  const uint32_t f = not_finite(w);
+  return w & ~((f - (f >> 15)) | f);
+}
+
 // LDS byte address.
 __device__ __forceinline__ uint32_t lds_u32(const void* p) {
   return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void*)p));

@@ -206,6 +206,7 @@ __device__ __forceinline__ void rows_body(const RowsArgs& a) {
 #pragma unroll
     for (int t = 0; t < DT; ++t) o[nb][t] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
+  bool sick = false;   // values that are not finite were cleared
   const bf16x2 ones = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
 
   // Keys k .. k + 31: pages j, j + 1 (a last single page stands in for its second, whose keys are not seen).
@@ -230,7 +231,6 @@ __device__ __forceinline__ void rows_body(const RowsArgs& a) {
       }
     }
     auto word_of = [&](int nb) { return WLDS ? w_lds[wave][nb][c] : seen_w[WLDS ? 0 : nb]; };
-    uint32_t bad = 0;   // bit r of lane row qd: the values of key 4 qd + r (r >= 4: 12 + 4 qd + r) are not all finite
     bf16x8 vop[DT];
     auto convert = [&]() {
       const uint32_t wa[4] = {pa.v[0].x, pa.v[0].y, pa.v[1].x, pa.v[1].y}, wb[4] = {pb.v[0].x, pb.v[0].y, pb.v[1].x, pb.v[1].y};
@@ -259,23 +259,14 @@ __device__ __forceinline__ void rows_body(const RowsArgs& a) {
           any |= not_finite(w[0]) | not_finite(w[1]) | not_finite(w[2]) | not_finite(w[3]);
         }
         if (__builtin_expect(__builtin_amdgcn_ballot_w64(any != 0) != 0, false)) {
-          // They must not meet weights of 0: cleared here, their products are added by themselves below.
-#pragma unroll
-          for (int t = 0; t < DT; ++t) {
-            const u32x4_t w = __builtin_bit_cast(u32x4_t, vop[t]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const uint32_t f = not_finite(w[i]);
-              bad |= ((f >> 15 & 1) | (f >> 31) << 1) << (2 * i);
-            }
-          }
-          for (int off = 1; off < 16; off <<= 1) bad |= __float_as_uint(xor_shfl(__uint_as_float(bad), off));
-          const uint32_t good = ~bad;
+          // They must not meet weights of 0: cleared here, and added after the last step to the rows that see them (any weight of an
+          // infinity is an infinity).
+          sick = true;
 #pragma unroll
           for (int t = 0; t < DT; ++t) {
             u32x4_t w = __builtin_bit_cast(u32x4_t, vop[t]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = mask_bf16x2(w[i], good >> (2 * i) & 1, good >> (2 * i + 1) & 1);
+            for (int i = 0; i < 4; ++i) w[i] = finite_or_zero(w[i]);
             vop[t] = __builtin_bit_cast(bf16x8, w);
           }
         }
@@ -343,31 +334,7 @@ __device__ __forceinline__ void rows_body(const RowsArgs& a) {
         ps = weights();
       }
       l_run[nb] += ps;
-      if constexpr (!FP4) {
-        if (__builtin_expect(__builtin_amdgcn_ballot_w64(bad != 0) != 0, false)) {
-          for (int qq = 0; qq < 4; ++qq) {
-            uint32_t left = __builtin_amdgcn_readlane(bad, 16 * qq);
-            while (left != 0) {
-              const int b = __builtin_ctz(left);
-              left &= left - 1;
-              const uint64_t lo = static_cast<uint64_t>(pw.y) << 32 | pw.x, hi = static_cast<uint64_t>(pw.w) << 32 | pw.z;
-              const uint32_t mine = static_cast<uint32_t>((b < 4 ? lo : hi) >> (16 * (b & 3))) << 16;
-              const float wt = __int_as_float(__builtin_amdgcn_ds_bpermute((16 * qq + c) << 2, static_cast<int>(mine)));
-              const int key = 4 * qq + (b & 3);
-              const bool sees = word_of(nb) >> (key + (b < 4 ? 0 : 16)) & 1;
-              const uint16_t* v = reinterpret_cast<const uint16_t*>(base + static_cast<size_t>(__builtin_amdgcn_readlane(pid, b < 4 ? j : min(j + 1, n_pg - 1))) * page_stride) +
-                                  kPageTokens * D + key;
-#pragma unroll
-              for (int t = 0; t < DT; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                  const float y = __uint_as_float(static_cast<uint32_t>(v[(16 * t + 4 * qd + r) * kPageTokens]) << 16);
-                  if (sees) o[nb][t][r] = __builtin_fmaf(wt, y, o[nb][t][r]);
-                }
-            }
-          }
-        }
-      } else {
+      if constexpr (FP4) {
         pw = make_uint4(pack_bf16x2(p[0] * vn[0], p[1] * vn[1]), pack_bf16x2(p[2] * vn[2], p[3] * vn[3]),
                         pack_bf16x2(p[4] * vn[4], p[5] * vn[5]), pack_bf16x2(p[6] * vn[6], p[7] * vn[7]));
       }
@@ -391,6 +358,31 @@ __device__ __forceinline__ void rows_body(const RowsArgs& a) {
     for (int j = 0; j < n_pg; j += 2) {
       const Page pa = load(j), pb = load(min(j + 1, n_pg - 1));
       step(pa, pb, j);
+    }
+  }
+
+  if constexpr (!FP4) {
+    if (__builtin_expect(sick, false)) {
+      const uint32_t* words = (const uint32_t*)meta_at<uint32_t>(a.meta, a.words_off) + mk.off;
+      for (int key = max(k_begin, mk.clear & ~31); key < k_end; ++key) {   // of the masked steps
+        const uint16_t* v = reinterpret_cast<const uint16_t*>(base + static_cast<size_t>(__builtin_amdgcn_readlane(pid, (key - k_begin) / kPageTokens)) * page_stride) +
+                            kPageTokens * D + key % kPageTokens;
+        uint32_t x[DT][4];
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) x[t][r] = v[(16 * t + 4 * qd + r) * kPageTokens];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          const int i = min((16 * nb + c) >> a.group_log2, cd.q_len - 1);
+          const bool sees = words[static_cast<size_t>(i) * mk.words + (key >> 5) - (mk.clear >> 5)] >> (key & 31) & 1;
+#pragma unroll
+          for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (sees && (x[t][r] & 0x7F80u) == 0x7F80u) o[nb][t][r] += __uint_as_float(x[t][r] << 16);
+        }
+      }
     }
   }
 

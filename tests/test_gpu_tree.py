@@ -149,11 +149,12 @@ def test_branches_do_not_meet(hq, hkv, d, n, fmt, bad):
 
 
 @pytest.mark.parametrize("hq,hkv,d,n", [(32, 8, 128, 8), (4, 2, 64, 20), (8, 8, 128, 100), (16, 8, 64, 130)])
-def test_value_of_a_branch_not_finite(hq, hkv, d, n):
-    """Only V is infinite, in one dim: that dim is infinite for the rows that see it, everything else is the oracle's."""
-    prefix = 30
+@pytest.mark.parametrize("prefix,back", [(30, None), (45, 1), (100, 3), (127, 40), (640, 30)])
+def test_value_of_a_branch_not_finite(hq, hkv, d, n, prefix, back):
+    """Only V is infinite, in one dim: that dim is infinite for the rows that see it (all of them, where it is a cached token's,
+    `back` tokens before the tree), everything else is the oracle's."""
     k, v = kv_tokens(SEED, 0, 1, 0, prefix + n, hkv, d)
-    sick = prefix + n // 3
+    sick = prefix + n // 3 if back is None else prefix - back
     well = v.clone()
     v[0, sick, :, 7] = float("inf")
     pool = _pool(hq, hkv, d)

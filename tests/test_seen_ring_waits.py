@@ -1,6 +1,5 @@
 """CPU: waits of the tiles of trees and cross attention over bf16 pages, read from the built library's own gfx950 code, by the scan of
-test_lds_ring_waits: at a step's barrier only the K reads of the next tile may be in flight. What a masked tile reads of the ring in
-addition (values that are not finite) has returned."""
+test_lds_ring_waits: at a step's barrier only the K reads of the next tile may be in flight."""
 import os
 import re
 
@@ -18,7 +17,7 @@ def test_no_read_of_a_retired_buffer_crosses_a_barrier(tmp_path):
             continue
         checked += 1
         d = int(m[1])
-        assert any(op == "ds_read_u16" or op.startswith("ds_read_u16") for _, op, _, _ in body)
+        assert any(op == "ds_read_b128" for _, op, _, _ in body)
         for pend in _pending(body):
             assert "w" not in pend, f"{name}: {pend}"
             regs = {r for r, _ in pend}
