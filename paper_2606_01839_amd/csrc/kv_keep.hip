@@ -7,7 +7,8 @@
 // sources' places and one for their bytes, a page; accepted drafts are one or two pages long.
 // V lies dimension-major, 32 bytes a dim and page: whole rows of a source page are loaded and the tokens picked from registers (a
 // 2-byte load for each token and dim keeps the address units busy for 41 of 85 us of 64 conversations, 32 layers, 8 kv heads). Of a page's rows
-// the half of 8 slots in front of the first that changes is neither read nor written.
+// the half of 8 slots in front of the first that changes is neither read nor written. 64 conversations, 32 layers, 8 kv heads: 44 us a
+// call (104 MB read, 108 written); one conversation of 4 layers 4.5.
 #include "device_common.hpp"
 #include "fp4.hpp"
 #include "kernels.hpp"

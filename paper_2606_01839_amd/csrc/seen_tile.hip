@@ -1,5 +1,7 @@
 // Attention of rows that are not a conversation's last tokens in causal order (host/seen.hpp), for many rows: the tiles of
-// attn_tile.hpp with words in place of the causal mask.
+// attn_tile.hpp with words in place of the causal mask. Bound by the matrix cores as those: 62% busy in texts of 100-3500 rows on
+// 600-9000 states (264 GFLOP, 251 us), 65% in trees of 130-250 tokens on 8k-40k (483 GFLOP, 496 us, an eighth of the tiles'
+// rows empty); by HBM where a tile's rows are few (64 trees of 32 tokens on 8k-32k 865 us, 5.3 TB/s).
 #include "attn_tile.hpp"
 
 namespace cs {
