@@ -293,7 +293,8 @@ cs_status cs_kv_append_tree(cs_pool* pool, const cs_rope* rope, int32_t n_convs,
  * bytes move as they are. Where the kept tokens are the first ones nothing moves.
  * After CS_EHIP the last n_last tokens are undefined, the lengths unchanged. Not under stream capture (CS_ESTATE).
  * Errors: CS_EINVAL (null, duplicate conversation, n_keep not in 0 .. n_last, keep not increasing in 0 .. n_last - 1),
- * CS_ENOENT, CS_ESTATE (n_last > length), CS_ENOMEM (more moved tokens than a metadata upload holds, some 250,000), CS_EHIP.
+ * CS_ENOENT, CS_ESTATE (n_last > length), CS_ENOMEM (more than one metadata upload holds, some 250,000 moved tokens or 20,000
+ * conversations; nothing is changed), CS_EHIP.
  */
 cs_status cs_kv_keep(cs_pool* pool, int32_t n_convs, const cs_conv* convs, const int32_t* n_last, const int32_t* n_keep,
                      const int32_t* keep, cs_stream stream);

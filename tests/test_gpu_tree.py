@@ -258,6 +258,34 @@ def test_append_at_tree_positions(hq, hkv, d, nl, ns, interleaved, rotary):
     pool.close()
 
 
+@pytest.mark.parametrize("convs_n", [400, 600])
+def test_append_of_many_trees(convs_n):
+    """More page chunks than one upload holds (some 21,800); 600 trees of 1024 tokens have more rows than an upload has positions for, so
+    their queries turn in the append's own launches."""
+    from paper_2606_01839_amd import Rope
+    n, d = 1024, 64
+    pool = _pool(1, 1, d, n_pages=convs_n * 65, max_convs=convs_n, max_pages=66)
+    convs = [pool.conv_create() for _ in range(convs_n)]
+    one = torch.randn((1, convs_n, 1, d), device="cuda").to(torch.bfloat16)
+    pool.kv_append_batch(convs, [1] * convs_n, one, one)   # trees begin in the middle of a page
+    g = torch.Generator(device="cuda").manual_seed(5)
+    k, q = (torch.randn((1, convs_n * n, 1, d), generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    parents = [tree(n, i % 7) for i in range(convs_n)]
+    depths = [so.depths(tree(n, i)) for i in range(7)]
+    qo = pool.kv_append_tree(convs, [n] * convs_n, parents, k, k, Rope(d), q=q)
+    f, amp = orope.frequencies(d, 10000.0)
+    for i in (0, 1, convs_n // 2, 335, 336, convs_n - 1):
+        rows = slice(i * n, (i + 1) * n)
+        gk, gv = pool.kv_read([convs[i]], [1], [n])
+        assert torch.equal(gv, k[:, rows])
+        for got, x in ((gk, k[:, rows]), (qo[:, rows], q[:, rows])):
+            xf = f64(x.cpu())
+            ref = orope.rotate(xf, 1 + depths[i % 7], f, amp)
+            tol = 2.0 ** -21 * 2 * np.abs(xf).max() + half_ulp_bf16(ref)
+            assert (np.abs(f64(got.cpu()) - ref) <= tol).all(), i
+    pool.close()
+
+
 def test_chain_append_is_append_rope():
     """A chain's positions are its slots: the same bits as kv_append_rope, in place for the queries."""
     from paper_2606_01839_amd import Rope
