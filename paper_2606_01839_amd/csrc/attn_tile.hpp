@@ -119,7 +119,8 @@ __device__ __forceinline__ void lds_wait_barrier() { asm volatile("s_waitcnt lgk
 // SEEN: the rows see what their words say (host/seen.hpp) in place of the keys up to their own: a tree's tokens, or every key.
 // Only tiles that reach past the keys that all rows see test bits, one word a row and 32 keys. There a value that is
 // not finite must not meet a weight of 0: it is cleared in the operands and added after the last tile to the rows that see it (any
-// weight of an infinity is an infinity).
+// weight of an infinity is an infinity). So are those behind the last key, which no row sees: what a failed append left in
+// the last page, and pages that stand in for those behind it.
 template <int D, int G, bool PRE, bool CHAIN, bool FP4 = false, bool SEEN = false>
 __device__ __forceinline__ void attn_fwd_block(const std::conditional_t<SEEN, SeenTileArgs, ExtendArgs>& a, const int block, const int dl) {
   constexpr int NW = 8;                   // waves: G query heads x (8 / G) blocks of 32 queries
@@ -540,7 +541,7 @@ __device__ __forceinline__ void attn_fwd_block(const std::conditional_t<SEEN, Se
     }
     l_run += ps;
     if constexpr (SEEN) {
-      if (partly && mk.words > 0) {
+      if (partly) {
         uint32_t any = 0;
 #pragma unroll
         for (int kt2 = 0; kt2 < 2; ++kt2)
