@@ -258,7 +258,7 @@ __device__ __forceinline__ void rows_body(const RowsArgs& a) {
 #pragma unroll
         for (int t = 0; t < DT; ++t) vop[t] = pages_v(pa.v[t], u32x2_t{0, 0});
       }
-      if (partly && mk.words > 0) {
+      if (partly) {
         uint32_t any = 0;
 #pragma unroll
         for (int t = 0; t < DT; ++t) {
@@ -267,7 +267,7 @@ __device__ __forceinline__ void rows_body(const RowsArgs& a) {
         }
         if (__builtin_expect(__builtin_amdgcn_ballot_w64(any != 0) != 0, false)) {
           // They must not meet weights of 0: cleared here, and added after the last step to the rows that see them (any weight of an
-          // infinity is an infinity).
+          // infinity is an infinity). No row sees those behind the last key, which a failed append may have left.
           sick = true;
 #pragma unroll
           for (int t = 0; t < DT; ++t) {
@@ -382,7 +382,7 @@ __device__ __forceinline__ void rows_body(const RowsArgs& a) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
           const int i = min((16 * nb + c) >> a.group_log2, cd.q_len - 1);
-          const bool sees = words[static_cast<size_t>(i) * mk.words + (key >> 5) - (mk.clear >> 5)] >> (key & 31) & 1;
+          const bool sees = key < mk.clear || (words[static_cast<size_t>(i) * mk.words + (key >> 5) - (mk.clear >> 5)] >> (key & 31) & 1);
 #pragma unroll
           for (int t = 0; t < DT; ++t)
 #pragma unroll

@@ -13,6 +13,7 @@ pytestmark = pytest.mark.gpu
 
 SEED = 2718
 TILES = [(4, 2, 64, 70), (8, 8, 128, 100), (16, 8, 64, 40), (32, 8, 128, 17), (8, 1, 128, 300)]   # more than 64 rows a kv head
+ROWS = [(4, 2, 64, 1), (32, 8, 128, 3), (8, 8, 128, 40), (16, 8, 64, 32), (32, 8, 128, 16), (32, 8, 64, 12)]   # 2 to 64
 LENS = [5, 16, 30, 64, 81, 100, 128, 333, 1000]   # 1 to 63 pages, of every remainder to four; whole last pages and others
 
 
@@ -51,6 +52,12 @@ def test_infinite_value_many_rows(hq, hkv, d, n, length):
     _infinity(hq, hkv, d, n, length)
 
 
+@pytest.mark.parametrize("length", LENS)
+@pytest.mark.parametrize("hq,hkv,d,n", ROWS)
+def test_infinite_value_few_rows(hq, hkv, d, n, length):
+    _infinity(hq, hkv, d, n, length)
+
+
 def _failed_append(hq, hkv, d, n, fmt, length, bad):
     """An append whose K and V are stored and whose queries' launch then fails: no conversation is longer, and attention is bit for
     bit what it was before."""
@@ -82,4 +89,12 @@ def _failed_append(hq, hkv, d, n, fmt, length, bad):
 @pytest.mark.parametrize("fmt", ["bf16", "fp4"])
 @pytest.mark.parametrize("hq,hkv,d,n", TILES)
 def test_failed_append_many_rows(hq, hkv, d, n, fmt, length, bad):
+    _failed_append(hq, hkv, d, n, fmt, length, bad)
+
+
+@pytest.mark.parametrize("bad", ["nan", "inf"])
+@pytest.mark.parametrize("length", [5, 30, 333])
+@pytest.mark.parametrize("fmt", ["bf16", "fp4"])
+@pytest.mark.parametrize("hq,hkv,d,n", ROWS)
+def test_failed_append_few_rows(hq, hkv, d, n, fmt, length, bad):
     _failed_append(hq, hkv, d, n, fmt, length, bad)
