@@ -42,8 +42,9 @@ PROFILES = os.path.join(ROOT, "profiles")
 # are unchanged (their SHA-256 is stored with the counters).
 KERNEL_SOURCES = {
     "decode_split": ["paper_2606_01839_amd/csrc/decode.hip", "paper_2606_01839_amd/csrc/decode_split.hpp",
-                     "paper_2606_01839_amd/csrc/device_common.hpp"],
-    "attn_fwd": ["paper_2606_01839_amd/csrc/attn_fwd.hip", "paper_2606_01839_amd/csrc/decode_split.hpp",
+                     "paper_2606_01839_amd/csrc/fp4.hpp", "paper_2606_01839_amd/csrc/device_common.hpp"],
+    "attn_fwd": ["paper_2606_01839_amd/csrc/attn_fwd.hip", "paper_2606_01839_amd/csrc/attn_tile.hpp",
+                 "paper_2606_01839_amd/csrc/decode_split.hpp", "paper_2606_01839_amd/csrc/fp4.hpp",
                  "paper_2606_01839_amd/csrc/device_common.hpp"],
     "kv_move": ["paper_2606_01839_amd/csrc/kv_move.hip", "paper_2606_01839_amd/csrc/device_common.hpp"],
 }
