@@ -5,6 +5,7 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import fp4 as o4
 from oracle import seen as so
 from tests.helpers import f64, kv_tokens, q_tokens
 from tests.seen_helpers import assert_within
@@ -56,6 +57,28 @@ def test_infinite_value_many_rows(hq, hkv, d, n, length):
 @pytest.mark.parametrize("hq,hkv,d,n", ROWS)
 def test_infinite_value_few_rows(hq, hkv, d, n, length):
     _infinity(hq, hkv, d, n, length)
+
+
+@pytest.mark.parametrize("length", [5, 81, 128, 1000])
+@pytest.mark.parametrize("hq,hkv,d,n", [x for x in TILES + ROWS if x[1] > 1])
+def test_value_over_4_bit_pages(hq, hkv, d, n, length):
+    """The last state's group of a kv head is NaN, and all dims of the heads that read it."""
+    pool = _pool(hq, hkv, d, "fp4")
+    k, v = kv_tokens(SEED, length, 1, 0, length, hkv, d)
+    well = v.clone()
+    v[0, length - 1, 1, 5] = float("inf")
+    c = pool.conv_create()
+    pool.kv_append(c, k.cuda(), v.cuda())
+    q = q_tokens(SEED, 1, 0, 0, n, hq, d)
+    out = pool.attn_cross([c], [n], 0, q.cuda()).cpu()
+    mine = slice(hq // hkv, 2 * (hq // hkv))
+    assert torch.isnan(out[:, mine]).all()
+    (kf, vf), qf = o4.held(f64(k[0]), f64(well[0])), f64(q)
+    see = np.ones((n, length), dtype=bool)
+    ref = so.attend(qf, kf, vf, see)
+    out[:, mine] = torch.from_numpy(ref).to(torch.bfloat16)[:, mine]
+    assert_within(out, qf, kf, vf, see, ref, "other heads", True)
+    pool.close()
 
 
 def _failed_append(hq, hkv, d, n, fmt, length, bad):
