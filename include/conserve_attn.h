@@ -18,8 +18,10 @@
  *    stream reaches the call. Host pointers: cs_conv arrays, q_lens, and the out-parameters.
  *  - Element type: bf16 (IEEE binary32 with the low 16 bits dropped) everywhere; accumulation fp32.
  *    A pool may hold K and V in 4 bits instead (cs_pool_create_as); what goes in and out stays bf16.
- *  - Append-then-attend: cs_kv_append is the only writer of a conversation's K/V. Attention calls (but for cs_attn_tree
- *    and cs_attn_cross) take queries for the LAST q_len positions of each conversation; query i of a conversation of
+ *  - Append-then-attend: a conversation's K/V are written by the append calls (cs_kv_append, its batched,
+ *    rotated and tree forms, the mixed steps), by cs_kv_unpack, which makes the conversation, and by
+ *    cs_kv_keep, which moves tokens within it; attention only reads them. Attention calls (but for
+ *    cs_attn_tree and cs_attn_cross) take queries for the LAST q_len positions of each conversation; query i of a conversation of
  *    length L sits at position p = L - q_len + i and sees keys 0..p (itself included). Softmax
  *    scale is exactly 1/sqrt(head_dim). Query head h reads KV head h / (n_q_heads / n_kv_heads).
  *  - Errors: every call validates all arguments before changing any state; on error it returns a
@@ -27,7 +29,9 @@
  *    aborts or throws across this ABI. CS_EHIP reports a failing HIP runtime call, CS_ENOMEM also host
  *    memory that ran out; an append that fails so still changes no length and no page (its reserved
  *    pages return to the free list); cs_mixed_step's append is complete when a later attention launch
- *    fails; after either the outputs of the failing call are undefined.
+ *    fails; after either the outputs of the failing call are undefined. What such an append stored behind a
+ *    conversation's end is seen by no row, but where its values are not finite, prefill and extend give
+ *    NaN until a later append has overwritten them.
  *  - Asynchrony: host metadata (lengths, page tables) is committed when the call returns; kernels
  *    and the small metadata uploads they need are enqueued on `stream` (a hipStream_t, 0 = null
  *    stream). No call synchronises the device, except that switching a pool to another stream
@@ -265,7 +269,9 @@ cs_status cs_attn_extend(cs_pool* pool, int32_t n_convs, const cs_conv* convs,
  * place of one token). The last q_lens[i] tokens of conversation i are a tree: parents[..], one for each query row in batch
  * order, is -1 (the token follows the last cached one) or the index of an earlier token of the same tree, counted from
  * its first. Row j sees the length - q_lens[i] cached tokens, its ancestors and itself, and no other branch: a NaN or infinity in
- * a branch it does not see (keys or values) does not reach it. A tree that is a chain (parents -1, 0, 1, ..) is cs_attn_extend.
+ * a branch it does not see (keys or values) does not reach it. An infinite value that a row sees makes that dim of it the same
+ * infinity, or NaN where it sees both signs or the key's weight underflows (below 2^-126 of the row's largest). A tree that is a chain
+ * (parents -1, 0, 1, ..) is cs_attn_extend.
  * At most CS_MAX_DRAFT tokens a tree. Pages of either format. Several lengths, and none, in one batch are fine.
  * q, out: device [sum(q_lens)][n_q_heads][head_dim] bf16. Deterministic and independent of page placement; a row's last bits
  * depend on the batch, as with cs_attn_extend. May be captured into a graph, as cs_attn_decode_batch_noalloc.
@@ -304,7 +310,7 @@ cs_status cs_kv_keep(cs_pool* pool, int32_t n_convs, const cs_conv* convs, const
  * context), appended like any tokens. No mask, no relation between a row and a position: any number of rows, more
  * than the conversation has tokens too, one for each of several hypotheses or a whole text. A conversation may appear several
  * times in a batch (rows of its entries are computed one by one; as one entry they share the reading). Rows of a conversation
- * without tokens are zeros. q, out, the result's bits, and capture: as cs_attn_tree.
+ * without tokens are zeros. q, out, the result's bits, infinite values, and capture: as cs_attn_tree.
  * Errors: CS_EINVAL (null, q_len < 0, too many rows), CS_ENOENT, CS_ERANGE (layer), CS_ENOMEM, CS_EHIP.
  */
 cs_status cs_attn_cross(cs_pool* pool, int32_t n_convs, const cs_conv* convs, const int32_t* q_lens, int32_t layer, const void* q,

@@ -739,8 +739,9 @@ cs_status append_impl(cs_pool* p, int32_t n, const cs_conv* convs, const int32_t
   // upload and launch has been issued. If one of those fails, or host memory runs out, the reserved pages go back to the
   // free list in their old order and nothing about the conversations changes. (Launches already
   // issued may have written the new tokens into the reserved pages and into unused slots past a
-  // conversation's end; no kernel reads those: attention masks keys past the length, pack writes
-  // zeros there, and the pages return to the free list.)
+  // conversation's end: the pages return to the free list, pack writes zeros there, and attention masks keys
+  // past the length. Values there that are not finite are cleared by decode, trees and cross attention; the tiles of prefill and
+  // extend multiply them by weights of 0, so rows of such a conversation are NaN until an append overwrites the slots.)
   std::vector<int32_t> slots(n), nn(n_new, n_new + n);
   std::vector<int64_t> old_lens(n);
   std::vector<size_t> old_pages(n);
@@ -1049,8 +1050,11 @@ cs_status run_seen(cs_pool* p, const std::vector<SeenEntry>& entries, bool all, 
                         [&] { return cs::launch_seen_empty(p->geom(), m, static_cast<int>(n), out, p->stream); });
     if (st != CS_OK) return st;
   }
-  // Both kinds in one batch take four launches one after the other: the few-row entries join the tiles where those hold more keys
-  // (16 trees of 17 to 100 tokens, 16 query and 8 kv heads, over 4-bit pages of 1k-9k: 72.7 us against 76).
+  // Both kinds in one batch take four launches one after the other: the few-row entries join the tiles where those hold more keys.
+  // Joined against apart, trees of 40 tokens beside trees of 6, 32 query and 8 kv heads of 128, half of the keys under each: 16 of
+  // 300-2000 tokens 46.0 us against 52.2, 16 of 1k-9k 73.0 against 78.4 (4-bit pages 73.2 against 72.4), 32 of 2k-9k 157 against 149 (129
+  // against 117), 64 of 8k-32k 989 against 972 (813 against 679). What joining saves is two launches; what it costs grows with the few-row
+  // entries' keys: from some 50,000 of them on it costs more.
   int64_t row_keys = 0, tile_keys = 0;
   for (const SeenEntry& x : rows) row_keys += x.len;
   for (const SeenEntry& x : tiles) tile_keys += x.len;

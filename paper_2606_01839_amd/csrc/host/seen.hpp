@@ -27,8 +27,8 @@ struct SeenItem {
 
 // Keys per wave of the rows kernel for a batch of conversations: the smallest multiple of 32 whose items (workgroups of
 // kDecodeSubSplits waves, one a CU, over all kv heads) fit one round of the CUs, or one and a half, or two, with items of at most twice a
-// CU's share of the keys; where there is none, 1024. Conversations of at most 512 tokens are one item (a pool that holds no
-// longer ones has no records). Items that just fill a round are the best that there is: 16 trees of 8
+// CU's share of the keys; where there is none, 1024. In a batch whose longest conversation has at most 512 tokens each is one item (a pool that
+// holds no longer ones has no records). Items that just fill a round are the best that there is: 16 trees of 8
 // on 1k-9k tokens (32 query and 8 kv heads of 128) take 38.4 us with 232 items, 46-49 with 304-560, 44-80 with 184-128; one of 12
 // on 100k 72.1 with 248, 85-120 with 320-3128. Beyond two rounds fewer items, with fewer records, are better: 64 on
 // 8k-32k 727 us with 1248, 744 with 1500; 200 on 300-5000 243 with 1600, 283 with 2248.

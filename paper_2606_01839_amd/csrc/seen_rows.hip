@@ -8,9 +8,9 @@
 // those of any magnitude keep their largest weight at 1.
 //
 // Bound: HBM where the cache is long. 64 conversations of 8k-32k tokens, 32 query and 8 kv heads of 128: 682 us for trees of one
-// token (6.70 TB/s, as the decode), 703 for 4, 729 for 8, 753 for 12, 778 for 16 (64 rows; as tiles 861); the matrix cores are 9%
+// token (6.70 TB/s, as the decode), 703 for 4, 729 for 8, 753 for 12, 796 for 16 (64 rows; as tiles 861); the matrix cores are 9%
 // busy at 28 rows. What the rows add is the join of an item's waves (a block of 16 rows 1 us at the end of an item) and
-// records. One tree of 16 tokens on 24.6k takes 26.4 us, of 4 19.6: start, loads in three bursts, join, merge launch 4.5.
+// records. One tree of 16 tokens on 24.6k takes 28.0 us, of 4 19.7: start, loads in three bursts, join, merge launch 4.5.
 // Over 4-bit pages 207 us for 4 tokens, 258 for 8, 393 for 16: arithmetic, two products' chains of each block.
 #include <cfloat>
 #include <cmath>
