@@ -960,7 +960,8 @@ cs_status run_seen_rows(cs_pool* p, const std::vector<SeenEntry>& entries, int32
       }
       w.blocks = (rows + 15) / 16;
       if (e == e0) break;
-      // (long items first need fewer records, then fewer entries do)
+      // (shorter items than 1024 keys a wave are at most 512 workgroups, whose records take a quarter of the room: where there is none
+      // the items are the longest already, and fewer entries need fewer records)
       split = split == 0 ? cs::rows_split(lens, g.n_kv_heads, cs::kCus) : 1024;
       plan = cs::decode_plan_of(slots, lens, split);
       size_t records = 0;

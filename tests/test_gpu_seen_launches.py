@@ -84,7 +84,8 @@ def test_one_entry_of_more_records_than_room():
     for call, see in ((lambda q: pool.attn_tree(convs, ns, [tree(n, i) for i, n in enumerate(ns)], 0, q), True),
                       (lambda q: pool.attn_cross(convs, ns, 0, q), False)):
         q = 4 * _randn((sum(ns), HQ, D), 9)
-        out = call(q)
+        out, launches = _launches(pool, lambda: call(q))
+        assert launches >= 4   # rows, the long one's tiles and their merge, rows and their merge
         for i in range(4):
             r0 = sum(ns[:i])
             long = i == 1
